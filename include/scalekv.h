@@ -59,12 +59,16 @@ typedef enum {
   SCALEKV_OK = 0,
   SCALEKV_ERR_INVALID_ARG = 1, /* null/misaligned pointer, negative size, length beyond capacity,
                                   window index out of range, overlapping source and destination */
-  SCALEKV_ERR_UNSUPPORTED = 2, /* head_dim or dtype the kernels are not built for */
+  SCALEKV_ERR_UNSUPPORTED = 2, /* head_dim, dtype or page size the kernels are not built for */
   SCALEKV_ERR_WORKSPACE = 3,   /* ws == NULL or ws_bytes below scalekv_workspace_bytes() */
   SCALEKV_ERR_HIP = 4          /* a kernel launch reported an error */
 } scalekv_status;
 
-typedef enum { SCALEKV_F32 = 0, SCALEKV_BF16 = 1 } scalekv_dtype;
+typedef enum {
+  SCALEKV_F32 = 0,
+  SCALEKV_BF16 = 1,
+  SCALEKV_E4M3 = 2 /* 8-bit floating point, of paged caches only */
+} scalekv_dtype;
 
 typedef struct {
   int32_t n_seq;    /* sequences (batch rows; classifier-free-guidance rows count separately) */
@@ -301,6 +305,117 @@ scalekv_status scalekv_select_positional(const scalekv_shape* shape, int32_t cac
  * gets b_uniform; the sum is exactly n_layer * b_uniform. */
 scalekv_status scalekv_pyramid_budgets(int32_t n_layer, int64_t b_uniform, int64_t b_last,
                                        int32_t* b);
+
+/* ---- A paged cache: rows of many sequences in pages of one pool, kept as they are or in 8 bits, and
+ * the attention that reads them where they are. ----
+ *
+ * A dense cache (scalekv_kv) has room for the longest length of every unit.  Under budgets that differ by layer and
+ * scale (Eq. 4), and with sequences of different lengths, most of that room is idle; pages are handed out by need,
+ * and one pool may serve all layers and sequences.  Row r of sequence s lies in page table[s][r / page_rows] at slot
+ * r % page_rows, the same for all heads.
+ *
+ * Elements.  The cache holds the type of the shape (fp32 or bf16), or SCALEKV_E4M3: an 8-bit code c (4 exponent
+ *   bits, 3 of mantissa, no infinities) for each element and one exponent k for each row and head, kept as the byte
+ *   k + 127; the element's value is c * 2^k.  Writing chooses the least k with max|x| <= 448 * 2^k over the finite
+ *   elements of the row, -117 <= k <= 120, and rounds x * 2^-k to the nearest code, ties to even: a relative error
+ *   of 2^-4 at most for elements above 2^(k-6), an absolute one of 2^(k-10) below.  Magnitudes above 240 * 2^120 are
+ *   held as that.  NaN and infinities become NaN.  Reading is exact.
+ * Heads.  n_kv_head divides the shape's n_head: query head h reads KV head h / (n_head / n_kv_head).
+ * New tokens.  Each sequence has up to max_new of them at a time; they are the LAST rows of its cache: with len[s]
+ *   rows (the new ones among them) and count[s] new tokens, token t has position len[s] - count[s] + t.  A token
+ *   whose position is negative is not in the cache: it is not written, and under a causal mask it sees nothing.
+ * Values in device memory (table, len, count, first, idx) are not seen by the host and may change between replays of
+ *   a captured call.  The kernels bring them into range, so that none of them leads out of a buffer: a length is
+ *   at most table_width * page_rows, a count at most max_new; a page that is not in [0, n_page) is not written and
+ *   reads as zeros; a token row outside [0, n_row) is not read (its query counts as zeros) or written.  A host copy of
+ *   them is checked by scalekv_pages_check.
+ * Pages may be shared by sequences (a common prefix) as long as nothing is written to them.  Calls that write
+ *   and read the same pages have to be in stream order. */
+typedef struct {
+  void* k;               /* device, [n_page, n_kv_head, page_rows, head_dim] of dtype, 16-byte aligned */
+  void* v;               /* likewise, with the strides of k */
+  uint8_t* k_scale;      /* device, [n_page, n_kv_head, page_rows]; SCALEKV_E4M3, otherwise ignored */
+  uint8_t* v_scale;      /* likewise, with the strides of k_scale */
+  int64_t page_stride;   /* elements between consecutive pages, >= n_kv_head * head_stride */
+  int64_t head_stride;   /* elements between consecutive heads of a page, >= page_rows * head_dim */
+  int64_t scale_page_stride, scale_head_stride; /* of the scales; >= n_kv_head * scale_head_stride, >= page_rows */
+  int32_t n_page;        /* pages of the pool, >= 1 */
+  int32_t n_kv_head;
+  int32_t page_rows;     /* rows of a page: 16, 32, 64, 128 or 256 */
+  int32_t dtype;         /* the shape's type or SCALEKV_E4M3 */
+  const int32_t* table;  /* device, [n_seq, table_width]: page numbers; entries behind a sequence's last are not used */
+  int32_t table_width;   /* >= 1; table_width * page_rows <= 2^30 */
+  const int32_t* len;    /* device, [n_seq]: rows of each sequence, the new tokens among them */
+} scalekv_pages;
+
+/* Rows of new tokens, in any order of sequence, head and token: element 0 of row i of head h of sequence s is
+ * ptr + s * seq_stride + h * head_stride + i * row_stride (elements, >= 0, multiples of 16 bytes; a row is contiguous). */
+typedef struct {
+  void* ptr; /* device, 16-byte aligned */
+  int64_t seq_stride, head_stride, row_stride;
+  int32_t n_row; /* rows of a sequence; of all sequences where they are packed one behind the other (seq_stride 0) */
+} scalekv_rows;
+
+/* The new tokens of each sequence s: count[s] rows from row first[s] on. */
+typedef struct {
+  int32_t max_new;      /* the most that any sequence has, >= 1 */
+  const int32_t* first; /* device, [n_seq]; NULL: 0 (one sequence's rows begin where its stride says) */
+  const int32_t* count; /* device, [n_seq]; NULL: max_new each */
+} scalekv_chunk;
+
+/* What a token at position p sees: rows j < len, and
+ *   causal: j <= p only;   window > 0: j > p - window, or j < n_sink, only. */
+typedef struct {
+  int32_t causal; /* 0 or 1; 0: the tokens of a map see all of it (Sec. 3.1) */
+  int32_t window; /* 0: none */
+  int32_t n_sink; /* first rows that stay visible outside the window (the sinks of Sec. 4.1's comparison) */
+} scalekv_mask;
+
+/* Writes k_new / v_new [n_kv_head heads] of the new tokens into their pages: quantised if the cache is
+ * SCALEKV_E4M3, else bit for bit.  No other row of the pool is touched.  Sequences that write must not share the
+ * pages written.  k_new / v_new must not overlap the pool, nor k and v (or the scales) each other:
+ * INVALID_ARG. */
+scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pages* pages,
+                                   const scalekv_rows* k_new, const scalekv_rows* v_new,
+                                   const scalekv_chunk* chunk, void* stream);
+
+/* Brings rows back into dense caches of shape->n_head heads (head h: KV head h / group), of the shape's type, exact.
+ * idx == NULL: rows [0, n_row) of every sequence; otherwise idx [S,H,n_row] (device) lists them, as
+ * scalekv_select writes them, and row t of the destination becomes row idx[t].  Destination rows whose source is not in
+ * [0, len[s]) are left as they are.  The destinations must not overlap each other or the pool. */
+scalekv_status scalekv_pages_read(const scalekv_shape* shape, const scalekv_pages* pages,
+                                  const int32_t* idx, int32_t n_row, const scalekv_kv* k_dst,
+                                  const scalekv_kv* v_dst, void* stream);
+
+/* Bytes of device workspace that scalekv_pages_attend needs for these sizes and this mask (0 where it needs
+ * none: then ws may be NULL).  Only sizes of `pages` are looked at.  mask NULL: every token sees every row.  *out is
+ * host memory. */
+scalekv_status scalekv_pages_workspace_bytes(const scalekv_shape* shape, const scalekv_pages* pages,
+                                             int32_t max_new, const scalekv_mask* mask, size_t* out);
+
+/* Attention of the new tokens over the pages, themselves included (write them first):
+ * out[t] = sum_j softmax_j(q_t.k_j * sm_scale) v_j over the rows that token t sees; a token that sees none, or rows
+ * of weight zero only, gets zeros.  q / out: n_head heads; `out` of rows behind a sequence's last token is not
+ * touched.  What a token does not see does not reach its output, whatever it holds.  fp32 softmax and sums; bf16 rounds
+ * the weights to bf16 before they multiply V, and an e4m3 row is multiplied as the bf16 (fp32) values it stands for.
+ * The key axis is split over workgroups where few rows meet long caches; sums are joined in a fixed order, results are
+ * reproducible bit for bit.  The workspace holds nothing between calls; calls that may overlap in time need
+ * one each.  out may lie exactly on q (same pointer and strides); any other overlap of `out` with q, the pool or
+ * ws, and rows of `out` that coincide (a stride of 0) -> INVALID_ARG. */
+scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pages* pages,
+                                    const scalekv_rows* q, const scalekv_chunk* chunk,
+                                    const scalekv_mask* mask, const scalekv_rows* out, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Host only: checks host copies of what the calls above read from device memory.  table [n_seq, table_width], len
+ * [n_seq]; count and first [n_seq] (NULL as in `chunk`, whose own pointers are not read; chunk NULL: nothing is new);
+ * n_row: of the tensors that hold the new tokens.  INVALID_ARG, and a message that names the entry, for: a
+ * length outside [0, table_width * page_rows]; a page in use outside [0, n_page); a count outside [0, min(max_new, len)];
+ * token rows outside [0, n_row); a page that receives new tokens and is used by another sequence or twice by one. */
+scalekv_status scalekv_pages_check(const scalekv_shape* shape, const scalekv_pages* pages,
+                                   const int32_t* table, const int32_t* len,
+                                   const scalekv_chunk* chunk, const int32_t* first,
+                                   const int32_t* count, int32_t n_row);
 
 /* Benchmark aid, not part of the method.  events: host array of 5 hipEvent_t
  * (created by the caller with timing enabled), or NULL to switch off.  While

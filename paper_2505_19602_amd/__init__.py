@@ -31,6 +31,12 @@ from .binding import (  # noqa: F401
     pyramid_budgets,
     policy_table,
     select_positional,
+    Pages,
+    pages_write,
+    pages_read,
+    pages_workspace_bytes,
+    pages_attend,
+    pages_check,
     MAX_WINDOW,
     MAX_ASI_SAMPLES,
     MAX_POOL,

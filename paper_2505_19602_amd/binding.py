@@ -35,7 +35,8 @@ _STATUS_SYMBOLS = (
     "scalekv_attend", "scalekv_step", "scalekv_step_static", "scalekv_step_stage_events",
     "scalekv_window_centroids", "scalekv_select_window", "scalekv_step_append_first",
     "scalekv_asi", "scalekv_drafter_set", "scalekv_allocate_budgets", "scalekv_select_positional",
-    "scalekv_pyramid_budgets", "scalekv_policy_table",
+    "scalekv_pyramid_budgets", "scalekv_policy_table", "scalekv_pages_write", "scalekv_pages_read",
+    "scalekv_pages_workspace_bytes", "scalekv_pages_attend", "scalekv_pages_check",
 )
 EXPORTED_SYMBOLS = _STATUS_SYMBOLS + ("scalekv_last_error", "scalekv_version")
 
@@ -559,3 +560,202 @@ def select_positional(shape: Shape, cache_len: int, n_sink: int, n_recent: int, 
                                            _ptr(idx), ctypes.byref(out), _stream()))
     assert out.value == keep, "the binding's shape check and the library disagree on keep"
     return int(out.value)
+
+
+# ---- the paged cache
+
+class _CPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("scale_page_stride", ctypes.c_int64),
+                ("scale_head_stride", ctypes.c_int64), ("n_page", ctypes.c_int32), ("n_kv_head", ctypes.c_int32),
+                ("page_rows", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("table_width", ctypes.c_int32), ("len", ctypes.c_void_p)]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("n_row", ctypes.c_int32)]
+
+
+class _CChunk(ctypes.Structure):
+    _fields_ = [("max_new", ctypes.c_int32), ("first", ctypes.c_void_p), ("count", ctypes.c_void_p)]
+
+
+class _CMask(ctypes.Structure):
+    _fields_ = [("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32)]
+
+
+_CACHE_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+
+
+def _on_device(t: torch.Tensor, name: str) -> torch.Tensor:
+    """Work goes onto the current device's stream: a tensor of another device would be used behind its back."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ScaleKVError(1, f"{name} is on {t.device}, it must be on the current device")
+    return t
+
+
+def _int_tensor(t: torch.Tensor, size, name: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(size) or not t.is_contiguous():
+        raise ScaleKVError(1, f"{name} must be a contiguous int32 tensor {list(size)}, got {t.dtype} {tuple(t.shape)}")
+    return _on_device(t, name)
+
+
+class Pages:
+    """scalekv_pages: a pool of pages and the sequences that use it.
+
+    k, v [n_page, n_kv_head, page_rows, d] (views with larger page and head strides are fine; the same strides for both)
+    of the shape's dtype or torch.float8_e4m3fn, which needs k_scale, v_scale [n_page, n_kv_head, page_rows] uint8 beside
+    it; table [S, width] int32: the pages of each sequence; lens [S] int32: its rows, new tokens among them.  Table and
+    lengths are read when a call's kernels run: they may be changed between calls, and between replays of a captured call.
+    """
+
+    __slots__ = ("k", "v", "table", "lens", "k_scale", "v_scale", "c")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        if k.dtype not in _CACHE_DTYPES:
+            raise ScaleKVError(2, f"pages of dtype {k.dtype}: not float32, bfloat16 or float8_e4m3fn")
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ScaleKVError(1, f"k {tuple(k.shape)} {k.dtype} and v {tuple(v.shape)} {v.dtype} must both be "
+                                  "[n_page, n_kv_head, page_rows, d]")
+        n_page, heads, rows, d = k.shape
+        strides = [self._strides(_on_device(t, name), rows * d, (n_page, heads), name) for t, name in ((k, "k"), (v, "v"))]
+        if strides[0] != strides[1]:
+            raise ScaleKVError(1, f"k and v have different strides: {k.stride()}, {v.stride()}")
+        scale_strides = [(0, 0), (0, 0)]
+        if k.dtype == torch.float8_e4m3fn:
+            for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                if t is None or t.dtype != torch.uint8 or tuple(t.shape) != (n_page, heads, rows):
+                    raise ScaleKVError(1, f"{name} must be a uint8 tensor {[n_page, heads, rows]} beside e4m3 pages")
+            scale_strides = [self._strides(_on_device(t, name), rows, (n_page, heads), name)
+                             for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+            if scale_strides[0] != scale_strides[1]:
+                raise ScaleKVError(1, f"k_scale and v_scale have different strides: {k_scale.stride()}, {v_scale.stride()}")
+        elif k_scale is not None or v_scale is not None:
+            raise ScaleKVError(1, f"pages of dtype {k.dtype} have no scales")
+        if table.dim() != 2:
+            raise ScaleKVError(1, f"table must be [S, width], got {tuple(table.shape)}")
+        _int_tensor(table, table.shape, "table")
+        _int_tensor(lens, table.shape[:1], "lens")
+        self.k, self.v, self.table, self.lens, self.k_scale, self.v_scale = k, v, table, lens, k_scale, v_scale
+        self.c = _CPages(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(),
+                         0 if v_scale is None else v_scale.data_ptr(), *strides[0], *scale_strides[0], n_page, heads, rows,
+                         _CACHE_DTYPES[k.dtype], table.data_ptr(), table.shape[1], lens.data_ptr())
+
+    @staticmethod
+    def _strides(t, unit, sizes, name):
+        """(page, head) strides; a dimension of one has none of its own.  unit: elements of a page of one head."""
+        if (t.dim() == 4 and (t.stride(3) != 1 or t.stride(2) != t.shape[3])) or (t.dim() == 3 and t.stride(2) != 1):
+            raise ScaleKVError(1, f"{name}: the rows of a page must be contiguous (strides {t.stride()})")
+        head = t.stride(1) if sizes[1] > 1 else unit
+        return (t.stride(0) if sizes[0] > 1 else max(sizes[1], 1) * head), head
+
+
+def _pages_of(shape: Shape, pages: Pages) -> Pages:
+    if pages.table.shape[0] != shape.n_seq or pages.k.shape[3] != shape.head_dim:
+        raise ScaleKVError(1, f"pages for {pages.table.shape[0]} sequences of head_dim {pages.k.shape[3]}, the shape has "
+                              f"{shape.n_seq} and {shape.head_dim}")
+    _on_device(pages.k, "pages")
+    return pages
+
+
+def _chunk(shape: Shape, rows: torch.Tensor, first, count, max_new, name: str) -> _CChunk:
+    if max_new is None:
+        if rows.dim() != 4 and shape.n_seq > 1:
+            raise ScaleKVError(1, f"max_new is needed where {name} holds the rows of several sequences")
+        max_new = rows.shape[2] if rows.dim() == 4 else rows.shape[0]
+    if rows.dim() == 3 and shape.n_seq > 1 and first is None:
+        raise ScaleKVError(1, f"first is needed where {name} holds the rows of several sequences")
+    for t, what in ((first, "first"), (count, "count")):
+        if t is not None:
+            _int_tensor(t, (shape.n_seq,), what)
+    return _CChunk(index(max_new), 0 if first is None else first.data_ptr(), 0 if count is None else count.data_ptr())
+
+
+def _rows(t: torch.Tensor, shape: Shape, heads: int, name: str) -> _CRows:
+    """[S, H, n, d], or packed [N, H, d], with any strides but for the rows' elements -> scalekv_rows."""
+    if t.dtype != shape.dtype:
+        raise ScaleKVError(1, f"{name} has dtype {t.dtype}, expected {shape.dtype}")
+    if t.dim() == 4:
+        want, dims = (shape.n_seq, heads, t.shape[2], shape.head_dim), (0, 1, 2)
+    elif t.dim() == 3:
+        want, dims = (t.shape[0], heads, shape.head_dim), (None, 1, 0)
+    else:
+        raise ScaleKVError(1, f"{name} has {t.dim()} dimensions, expected [S,H,n,d] or [N,H,d]")
+    if tuple(t.shape) != want:
+        raise ScaleKVError(1, f"{name} has shape {tuple(t.shape)}, expected {want}")
+    if t.stride(-1) != 1:
+        raise ScaleKVError(1, f"{name}: rows must be contiguous (strides {t.stride()})")
+    _on_device(t, name)
+    strides = [0 if x is None or t.shape[x] == 1 else t.stride(x) for x in dims]   # a dimension of one has none of its own
+    return _CRows(t.data_ptr(), *strides, t.shape[dims[2]])
+
+
+def pages_write(shape: Shape, pages: Pages, k_new: torch.Tensor, v_new: torch.Tensor,
+                first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                max_new: Optional[int] = None) -> None:
+    """scalekv_pages_write: rows of new tokens, [S, KV heads, n, d] or packed [N, KV heads, d], into their pages."""
+    _pages_of(shape, pages)
+    heads = pages.k.shape[1]
+    k, v = _rows(k_new, shape, heads, "k_new"), _rows(v_new, shape, heads, "v_new")
+    cs, chunk = shape.c(), _chunk(shape, k_new, first, count, max_new, "k_new")
+    if k_new.dim() != v_new.dim():
+        raise ScaleKVError(1, "k_new and v_new must both be packed or not")
+    _check(lib().scalekv_pages_write(ctypes.byref(cs), ctypes.byref(pages.c), ctypes.byref(k), ctypes.byref(v),
+                                     ctypes.byref(chunk), _stream()))
+
+
+def pages_read(shape: Shape, pages: Pages, idx: Optional[torch.Tensor], n_row: int, k_dst: torch.Tensor,
+               v_dst: torch.Tensor) -> None:
+    """scalekv_pages_read: rows [0, n_row), or those that idx [S,H,n_row] int32 lists, into caches [S,H,capacity,d]."""
+    _pages_of(shape, pages)
+    n_row = index(n_row)
+    _idx_tensor(idx, shape, n_row, "idx")
+    if idx is not None:
+        _on_device(idx, "idx")
+    cs, a, b = shape.c(), _kv(_on_device(k_dst, "k_dst"), shape, "k_dst"), _kv(_on_device(v_dst, "v_dst"), shape, "v_dst")
+    _check(lib().scalekv_pages_read(ctypes.byref(cs), ctypes.byref(pages.c), _ptr(idx), n_row, ctypes.byref(a),
+                                    ctypes.byref(b), _stream()))
+
+
+def pages_workspace_bytes(shape: Shape, pages: Pages, max_new: int, causal: bool = False, window: int = 0,
+                          n_sink: int = 0) -> int:
+    """scalekv_pages_workspace_bytes: device bytes that pages_attend needs for chunks of up to max_new tokens."""
+    out, cs, mask = ctypes.c_size_t(0), shape.c(), _CMask(int(bool(causal)), index(window), index(n_sink))
+    _check(lib().scalekv_pages_workspace_bytes(ctypes.byref(cs), ctypes.byref(pages.c), index(max_new), ctypes.byref(mask),
+                                               ctypes.byref(out)))
+    return int(out.value)
+
+
+def pages_attend(shape: Shape, pages: Pages, q: torch.Tensor, out: torch.Tensor, ws: Optional[torch.Tensor],
+                 causal: bool = False, window: int = 0, n_sink: int = 0, first: Optional[torch.Tensor] = None,
+                 count: Optional[torch.Tensor] = None, max_new: Optional[int] = None) -> None:
+    """scalekv_pages_attend: q, out [S,H,n,d] or packed [N,H,d]; the new tokens attend over the rows of their sequences,
+    themselves included.  causal: up to a token's own position; window: only the last `window` of those, and the
+    first n_sink rows of the cache."""
+    _pages_of(shape, pages)
+    cq, co = _rows(q, shape, shape.n_head, "q"), _rows(out, shape, shape.n_head, "out")
+    if q.dim() != out.dim():
+        raise ScaleKVError(1, "q and out must both be packed or not")
+    cs, chunk = shape.c(), _chunk(shape, q, first, count, max_new, "q")
+    mask = _CMask(int(bool(causal)), index(window), index(n_sink))
+    wp, wb = _ws(ws)
+    if ws is not None and ws.numel():
+        _on_device(ws, "ws")
+    _check(lib().scalekv_pages_attend(ctypes.byref(cs), ctypes.byref(pages.c), ctypes.byref(cq), ctypes.byref(chunk),
+                                      ctypes.byref(mask), ctypes.byref(co), wp, wb, _stream()))
+
+
+def pages_check(shape: Shape, pages: Pages, table: Sequence[Sequence[int]], lens: Sequence[int],
+                first: Optional[Sequence[int]] = None, count: Optional[Sequence[int]] = None,
+                max_new: Optional[int] = None, n_row: int = 0) -> None:
+    """scalekv_pages_check: host copies of the table, the lengths and (with max_new) what is new, against the sizes of
+    `pages`; n_row: token rows of a sequence (packed: of all).  Raises what the kernels would skip or read as zeros."""
+    cs, width = shape.c(), pages.table.shape[1]
+    if len(table) != shape.n_seq or any(len(r) != width for r in table) or len(lens) != shape.n_seq or             any(x is not None and len(x) != shape.n_seq for x in (first, count)):
+        raise ScaleKVError(1, f"expected table [{shape.n_seq}][{width}] and {shape.n_seq} lengths, firsts and counts")
+    ints = lambda x: None if x is None else (ctypes.c_int32 * len(x))(*[index(i) for i in x])
+    chunk = None if max_new is None else ctypes.byref(_CChunk(index(max_new), 0, 0))
+    _check(lib().scalekv_pages_check(ctypes.byref(cs), ctypes.byref(pages.c), ints([i for r in table for i in r]), ints(lens),
+                                     chunk, ints(first), ints(count), index(n_row)))

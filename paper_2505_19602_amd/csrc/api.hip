@@ -9,7 +9,7 @@
 #include <cmath>
 #include <vector>
 
-#include "../../include/scalekv.h"
+#include "api_checks.h"
 #include "common.h"
 
 using namespace scalekv;
@@ -19,6 +19,10 @@ namespace {
 thread_local char g_err[256] = "no error";
 thread_local void** g_stage_events = nullptr;  // benchmark hook, see scalekv_step_stage_events
 
+}  // namespace
+
+namespace scalekv {
+
 scalekv_status fail(scalekv_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -27,80 +31,9 @@ scalekv_status fail(scalekv_status st, const char* fmt, ...) {
   return st;
 }
 
-scalekv_status hip_fail(hipError_t e, const char* what) {
-  return fail(SCALEKV_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
+}  // namespace scalekv
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int elem_bytes(const scalekv_shape* s) { return s->dtype == SCALEKV_F32 ? 4 : 2; }
-
-float resolve_scale(const scalekv_shape* s) {
-  return s->sm_scale > 0.f ? s->sm_scale : 1.0f / sqrtf((float)s->head_dim);
-}
-
-scalekv_status check_shape(const scalekv_shape* s) {
-  if (!s) return fail(SCALEKV_ERR_INVALID_ARG, "shape is NULL");
-  if (s->n_seq <= 0 || s->n_head <= 0)
-    return fail(SCALEKV_ERR_INVALID_ARG, "n_seq and n_head must be positive (got %d, %d)",
-                s->n_seq, s->n_head);
-  if ((long long)s->n_seq * s->n_head > 65535)
-    return fail(SCALEKV_ERR_UNSUPPORTED, "n_seq * n_head = %lld exceeds 65535",
-                (long long)s->n_seq * s->n_head);
-  if (s->dtype != SCALEKV_F32 && s->dtype != SCALEKV_BF16)
-    return fail(SCALEKV_ERR_UNSUPPORTED, "dtype %d is neither SCALEKV_F32 nor SCALEKV_BF16",
-                s->dtype);
-  if (s->head_dim != 64 && s->head_dim != 128)
-    return fail(SCALEKV_ERR_UNSUPPORTED, "head_dim %d is not 64 or 128", s->head_dim);
-  if (!(s->sm_scale == s->sm_scale))
-    return fail(SCALEKV_ERR_INVALID_ARG, "sm_scale is NaN");
-  return SCALEKV_OK;
-}
-
-// rows * head_dim must fit int32 (kernels index a unit with 32-bit offsets in places)
-scalekv_status check_rows(const scalekv_shape* s, long long rows, const char* name) {
-  if (rows < 0) return fail(SCALEKV_ERR_INVALID_ARG, "%s is negative (%lld)", name, rows);
-  if (rows * s->head_dim > 0x7fffffffLL)
-    return fail(SCALEKV_ERR_UNSUPPORTED, "%s = %lld rows is too large", name, rows);
-  return SCALEKV_OK;
-}
-
-scalekv_status check_kv(const scalekv_shape* s, const scalekv_kv* kv, int rows_needed,
-                        const char* name) {
-  if (!kv) return fail(SCALEKV_ERR_INVALID_ARG, "%s is NULL", name);
-  if (!kv->ptr) return fail(SCALEKV_ERR_INVALID_ARG, "%s.ptr is NULL", name);
-  if (!aligned16(kv->ptr)) return fail(SCALEKV_ERR_INVALID_ARG, "%s.ptr is not 16-byte aligned", name);
-  if (kv->capacity < 0) return fail(SCALEKV_ERR_INVALID_ARG, "%s.capacity is negative", name);
-  if (rows_needed > kv->capacity)
-    return fail(SCALEKV_ERR_INVALID_ARG, "%s: %d rows needed but capacity is %d", name,
-                rows_needed, kv->capacity);
-  const long long unit = (long long)kv->capacity * s->head_dim;
-  const int epv = 16 / elem_bytes(s);
-  if (kv->head_stride < unit || kv->head_stride % epv)
-    return fail(SCALEKV_ERR_INVALID_ARG,
-                "%s.head_stride %lld must be >= capacity*head_dim (%lld) and a multiple of %d",
-                name, (long long)kv->head_stride, unit, epv);
-  if (kv->seq_stride < kv->head_stride * s->n_head || kv->seq_stride % epv)
-    return fail(SCALEKV_ERR_INVALID_ARG,
-                "%s.seq_stride %lld must be >= n_head*head_stride and a multiple of %d", name,
-                (long long)kv->seq_stride, epv);
-  return SCALEKV_OK;
-}
-
-scalekv_status check_dense(const void* p, bool required, const char* name) {
-  if (!p) return required ? fail(SCALEKV_ERR_INVALID_ARG, "%s is NULL", name) : SCALEKV_OK;
-  if (!aligned16(p)) return fail(SCALEKV_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-  return SCALEKV_OK;
-}
-
-// byte range [lo, hi) spanned by a cache
-void kv_span(const scalekv_shape* s, const scalekv_kv* kv, uintptr_t* lo, uintptr_t* hi) {
-  const long long e = elem_bytes(s);
-  *lo = reinterpret_cast<uintptr_t>(kv->ptr);
-  *hi = *lo + (uintptr_t)(((long long)(s->n_seq - 1) * kv->seq_stride +
-                           (long long)(s->n_head - 1) * kv->head_stride +
-                           (long long)kv->capacity * s->head_dim) * e);
-}
+namespace {
 
 bool overlaps(const scalekv_shape* s, const scalekv_kv* a, const scalekv_kv* b) {
   uintptr_t al, ah, bl, bh;
@@ -194,18 +127,6 @@ scalekv_status make_extras(const int32_t* forced, int n_forced, int pool_w, int 
   }
   return SCALEKV_OK;
 }
-
-#define SCALEKV_TRY(expr)                       \
-  do {                                          \
-    scalekv_status _st = (expr);                \
-    if (_st != SCALEKV_OK) return _st;          \
-  } while (0)
-
-#define SCALEKV_HIP(expr, what)                 \
-  do {                                          \
-    hipError_t _e = (expr);                     \
-    if (_e != hipSuccess) return hip_fail(_e, what); \
-  } while (0)
 
 }  // namespace
 

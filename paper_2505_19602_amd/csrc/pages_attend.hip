@@ -1,0 +1,653 @@
+// Attention of a chunk of new tokens over a paged cache (bf16, fp32, or e4m3 with a power-of-two scale to each row), with
+// a causal mask, a sliding window and first rows that stay visible.
+//
+// out_t = sum_j softmax_j(q_t . k_j * sm_scale) v_j over the rows j that token t sees, in one pass over the keys with the
+// running maximum and sum of the softmax.  The query rows of a workgroup are those of ONE KV head, (token, query head of
+// the group) in this order, so that the heads that share a row of the cache read it together: a single token of a group of
+// eight heads is eight rows.
+//
+// Products, transposed as in the dense kernels: S^T[key][row] = K Q^T with K from LDS and Q in registers, O^T[channel][row]
+// += V^T P^T with V^T from LDS and P^T in the registers that the first product left it in; a lane owns a query row (of each
+// tile of 16), its softmax statistics are scalars of the lane.  bf16: MFMA 16x16x32, blocks of 32 keys, key order and LDS
+// swizzle as in attend_pipe.hip.  fp32: MFMA 16x16x4, blocks of 16 keys.
+//
+// Tiles.  All waves bring in a tile of keys: whole rows, 16 bytes a lane, through registers into LDS, where e4m3 becomes
+// what the products take (exactly: four significant bits and a power of two), rows that no query row of the workgroup sees
+// become zeros, and the rows of the tile after it are requested before this one is worked on, their pages' numbers one
+// tile earlier still.  Waves either split the query rows (chunks) or the blocks of a tile (few rows), and in the latter
+// case join their results through LDS.  Where that leaves the chip idle the keys are split over workgroups as well; their
+// results go to the workspace, and pages_join_kernel adds them up.  A workgroup walks the tiles that its rows can see:
+// those of the first rows, then those from the window's first row on.
+//
+// Masked keys.  A weight of zero does not hide a value that is infinite or NaN from the product.  Rows hidden from all rows
+// of the workgroup are zeros in LDS; in the few tiles that some of its rows see and others do not (`edge`), values that
+// are not finite are taken out of the tile, remembered, and added for the rows that do see them (`add_odd`).
+#include "pages.h"
+
+namespace scalekv {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+
+constexpr int kThreads = 256;
+
+// TYPE: of queries, output and arithmetic; WQ: waves that split the query rows; RT: tiles of 16 query rows to a wave.
+template <int TYPE, bool Q8, int D, int WQ, int RT>
+struct Form {
+  static constexpr bool kBf16 = TYPE == kTypeBf16;
+  static constexpr int kElem = kBf16 ? 2 : 4;
+  static constexpr int WK = 4 / WQ;                      // waves that split the keys of a tile
+  static constexpr int kBlock = kBf16 ? 32 : 16;         // keys of a block
+  static constexpr int kBlocks = WK > 1 ? 1 : kBf16 ? 2 : 4;  // blocks of a tile to a wave
+  static constexpr int TN = kBlock * kBlocks * WK;       // keys of a tile
+  static constexpr int kKeyTiles = kBlock / 16;
+  static constexpr int kRowBytes = D * kElem;            // in LDS
+  static constexpr int kTileBytes = TN * kRowBytes;
+  static constexpr int kStages = WK == 1 && kBf16 ? 2 : 1;
+  static constexpr int kSlabs = kRowBytes / 64;          // 16-byte operands of a query row that a lane holds
+  static constexpr int kChans = D / 16;                  // 16-channel blocks of the output
+  static constexpr int kSrcRow = Q8 ? D : kRowBytes;     // bytes of a cached row
+  static constexpr int kSrcChunks = kSrcRow / 16;
+  static constexpr int kVecs = TN * kSrcChunks / kThreads;  // 16-byte vectors of a tile of K, or of V, to a thread
+  static constexpr int kRows = 16 * RT * WQ;             // query rows of a workgroup
+  static constexpr int kJoinBytes = WK > 1 ? (WK - 1) * 64 * RT * (kChans * 16 + 8) : 0;
+  static constexpr int kLds = 2 * kStages * kTileBytes > kJoinBytes ? 2 * kStages * kTileBytes : kJoinBytes;
+  // chunk c of row r sits in slot c ^ k_flip(r) of a K row, c ^ v_flip(r) of a V row
+  __device__ static constexpr int k_flip(int r) {
+    if (!kBf16) return r & 15;
+    const int high = (r >> 4 & 1) | (r >> 3 & 1) << 1;
+    return D == 128 ? (r & 3) | high << 2 : (r >> 1 & 1) | high << 1;
+  }
+  __device__ static constexpr int v_flip(int r) {
+    if (!kBf16) return r & 15;
+    return D == 128 ? (r & 3) << 1 | (r >> 4 & 1) << 3 : (r >> 1 & 1) << 1 | (r >> 4 & 1) << 2;
+  }
+};
+
+struct AttendArgs {
+  PagesView c;
+  RowsView q, out;
+  ChunkView chunk;
+  MaskView mask;
+  int n_seq, group, n_row_group, n_split, n_wg;
+  float scale_log2e, no_max;
+  float *part, *stat;  // partial sums [row][split][D], their {maximum, sum} [row][split][2]
+};
+
+// sixteen codes of a row with its scale, as the products take them
+__device__ __forceinline__ void widen(const u32x4& x, float s, u32x4 (&y)[2]) {  // bf16
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i / 2][i % 2 * 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], s, false));
+    y[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], s, true));
+  }
+}
+__device__ __forceinline__ void widen(const u32x4& x, float s, u32x4 (&y)[4]) {  // fp32
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], true);
+    y[i][0] = __float_as_uint(lo[0] * s);
+    y[i][1] = __float_as_uint(lo[1] * s);
+    y[i][2] = __float_as_uint(hi[0] * s);
+    y[i][3] = __float_as_uint(hi[1] * s);
+  }
+}
+// zeros in the place of what is not finite; whether there was any
+template <bool BF16>
+__device__ __forceinline__ bool take_odd(u32x4& x) {
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+      odd |= lo || hi;
+      x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    } else {
+      const bool it = (x[i] & 0x7f800000u) == 0x7f800000u;
+      odd |= it;
+      x[i] = it ? 0u : x[i];
+    }
+  }
+  return odd;
+}
+
+template <int TYPE, bool Q8, int D, int WQ, int RT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void pages_attend_kernel(AttendArgs a) {
+  using F = Form<TYPE, Q8, D, WQ, RT>;
+  constexpr bool BF16 = F::kBf16;
+  constexpr int TN = F::TN, KT = F::kKeyTiles, NSL = F::kSlabs, NCB = F::kChans, NV = F::kVecs;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ unsigned odd_rows[2][TN / 32];  // of the tile in each stage: rows with values that are not finite
+  const PagesView& c = a.c;
+
+  // ---- which query rows, which tiles
+  const int wg = xcd_order(SCALEKV_WG_X, a.n_wg);
+  const int split = wg % a.n_split, row_group = wg / a.n_split % a.n_row_group, unit = wg / a.n_split / a.n_row_group;
+  const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wq = wave % WQ, wk = wave / WQ;
+  const int len = pages_len(c, seq), count = chunk_count(a.chunk, seq);
+  const int n_rows = count * a.group, first_row = row_group * F::kRows;
+  if (first_row >= n_rows) return;  // (the rows of a split that are never written are not joined either)
+  const int pos0 = len - count;     // position of the first new token
+  // positions of the first and the last token of the workgroup, and of the wave
+  const int last_row = min(first_row + F::kRows, n_rows) - 1;
+  const int p_lo = pos0 + first_row / a.group, p_hi = pos0 + last_row / a.group;
+  const bool window = a.mask.window > 0;
+  auto end_of = [&](int p) { return a.mask.causal ? min(len, p + 1) : len; };        // rows from here on are hidden,
+  auto begin_of = [&](int p) { return window ? p - a.mask.window + 1 : -0x7fffffff; };  // those before too, but
+  const int sinks = window ? a.mask.n_sink : 0;                                        // the first of all
+  const int hi = end_of(p_hi), lo = begin_of(p_lo);
+  const int sink_tiles = (max(min(sinks, hi), 0) + TN - 1) / TN;
+  const int from_tile = max(max(lo, 0) / TN, sink_tiles), n_tile_all = sink_tiles + max((hi + TN - 1) / TN - from_tile, 0);
+  auto key0_of = [&](int t) { return (t < sink_tiles ? t : from_tile + t - sink_tiles) * TN; };  // first key of tile t
+  const int per = (n_tile_all + a.n_split - 1) / a.n_split;
+  const int t0 = min(split * per, n_tile_all), t1 = min(t0 + per, n_tile_all);
+
+  // ---- the query rows of this lane
+  const int wave_row = first_row + wq * (16 * RT);
+  int q_end[RT], q_begin[RT], q_row[RT];
+  u32x4 qf[RT][NSL];
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+    const int r = min(wave_row + 16 * b + i, n_rows - 1);
+    const int t = r / a.group, head = kv * a.group + (r - t * a.group);
+    q_row[b] = r;
+    q_end[b] = end_of(pos0 + t);
+    q_begin[b] = begin_of(pos0 + t);
+    const long long at = (long long)chunk_first(a.chunk, seq) + t;
+    const u32x4* src = (const u32x4*)(a.q.p + seq * a.q.seq + head * a.q.head + at * a.q.row);
+    const bool there = at >= 0 && at < a.q.n_row;
+#pragma unroll
+    for (int sl = 0; sl < NSL; ++sl) qf[b][sl] = there ? src[4 * sl + g] : u32x4{0, 0, 0, 0};
+  }
+  // what all rows of the wave see, and what all rows of the workgroup do: [begin, end) and the first `sinks`
+  const int w_lo = pos0 + min(wave_row, n_rows - 1) / a.group;
+  const int w_hi = pos0 + min(wave_row + 16 * RT - 1, n_rows - 1) / a.group;
+  const int w_end = end_of(w_lo), w_begin = begin_of(w_hi);
+  const int all_end = end_of(p_lo), all_begin = begin_of(p_hi);
+
+  // ---- tiles: a thread's vectors of a tile lie kThreads vectors apart
+  int page[NV];
+  u32x4 kr[NV], vr[NV];
+  uint8_t ks[NV], vs[NV];
+  const int ld_row = tid / F::kSrcChunks, ld_chunk = tid % F::kSrcChunks;
+  constexpr int kRowsApart = kThreads / F::kSrcChunks;
+  const int32_t* const table = c.table + (long long)seq * c.width;
+  const long long kv_ofs = kv * c.head, kv_scale = kv * c.scale_head;
+  auto visible_here = [&](int pos) { return pos < hi && (pos >= lo || pos < sinks); };
+  auto ask_pages = [&](int t) __attribute__((always_inline)) {
+    const int key0 = key0_of(t);
+#pragma unroll
+    for (int p = 0; p < NV; ++p) {
+      const int pos = key0 + ld_row + p * kRowsApart;
+      page[p] = -1;
+      if (t < t1 && visible_here(pos)) page[p] = table[pos >> c.page_shift];
+    }
+  };
+  auto ask_rows = [&](int t) __attribute__((always_inline)) {
+    const int key0 = key0_of(t);
+#pragma unroll
+    for (int p = 0; p < NV; ++p) {
+      const int slot = (key0 + ld_row + p * kRowsApart) & ((1 << c.page_shift) - 1);
+      kr[p] = vr[p] = u32x4{0, 0, 0, 0};
+      ks[p] = vs[p] = 127;
+      if ((unsigned)page[p] < (unsigned)c.n_page) {
+        const long long at = page[p] * c.page + kv_ofs + slot * F::kSrcRow + 16 * ld_chunk;
+        kr[p] = *(const u32x4*)(c.k + at);
+        vr[p] = *(const u32x4*)(c.v + at);
+        if constexpr (Q8) {
+          const long long scale_at = page[p] * c.scale_page + kv_scale + slot;
+          ks[p] = c.k_scale[scale_at];
+          vs[p] = c.v_scale[scale_at];
+        }
+      }
+    }
+  };
+  // some rows of the workgroup see a key of tile t that others do not
+  auto is_edge = [&](int t) {
+    const int key0 = key0_of(t), end = min(key0 + TN, hi);
+    return end > all_end || (window && max(key0, lo) < min(all_begin, end) && max(key0, sinks) < min(all_begin, end));
+  };
+  auto store_rows = [&](int t, int stage) __attribute__((always_inline)) {
+    unsigned char* const k_lds = smem + stage * F::kTileBytes;
+    unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
+    const bool edge = is_edge(t);
+    constexpr int kOut = Q8 ? F::kElem : 1;  // vectors in LDS for one of the cache
+#pragma unroll
+    for (int p = 0; p < NV; ++p) {
+      const int row = ld_row + p * kRowsApart;
+      u32x4 x[kOut], y[kOut];
+      if constexpr (Q8) {
+        widen(kr[p], __uint_as_float((unsigned)ks[p] << 23), x);
+        widen(vr[p], __uint_as_float((unsigned)vs[p] << 23), y);
+      } else {
+        x[0] = kr[p];
+        y[0] = vr[p];
+      }
+      if (edge) {
+        bool odd = false;
+#pragma unroll
+        for (int w = 0; w < kOut; ++w) odd |= take_odd<BF16>(y[w]);
+        if (odd) atomicOr(&odd_rows[stage][row / 32], 1u << (row % 32));
+      }
+#pragma unroll
+      for (int w = 0; w < kOut; ++w) {
+        const int chunk = ld_chunk * kOut + w;
+        *(u32x4*)(k_lds + row * F::kRowBytes + 16 * (chunk ^ F::k_flip(row))) = x[w];
+        *(u32x4*)(v_lds + row * F::kRowBytes + 16 * (chunk ^ F::v_flip(row))) = y[w];
+      }
+    }
+  };
+
+  // ---- state of the rows
+  f32x4 o[RT][NCB];
+  float m_run[RT], l_run[RT];  // largest logit (the same in the four lanes of a row), this lane's share of the sum
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+#pragma unroll
+    for (int x = 0; x < NCB; ++x) o[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[b] = a.no_max;
+    l_run[b] = 0.f;
+  }
+  // key of register v of key tile t, in a block
+  auto key_of = [&](int t, int v) { return BF16 ? 16 * (g & 1) + 8 * (g >> 1) + 4 * t + v : 4 * g + v; };
+
+  // Values that are not finite in rows of an edge tile, for the query rows that see them; w: weights of the block.
+  auto add_odd = [&](int key0, int block, unsigned rows, const float (&w)[RT][4 * KT]) {
+    for (int x = 0; x < 4 * KT; ++x)
+      for (int from = 0; from < 4; ++from) {
+        const int key = BF16 ? 16 * (from & 1) + 8 * (from >> 1) + x : 4 * from + x;
+        if (!(rows >> key & 1)) continue;
+        const int pos = key0 + block * F::kBlock + key, slot = pos & ((1 << c.page_shift) - 1);
+        const int pg = table[pos >> c.page_shift];  // (in the pool: its rows are not all zeros)
+        const unsigned char* src = c.v + (pg * c.page + kv_ofs + slot * F::kSrcRow);
+        float scale = 1.f;
+        if constexpr (Q8) scale = __uint_as_float((unsigned)c.v_scale[pg * c.scale_page + kv_scale + slot] << 23);
+#pragma unroll
+        for (int b = 0; b < RT; ++b) {
+          float weight = 0.f;
+#pragma unroll
+          for (int y = 0; y < 4 * KT; ++y) weight = y == x ? w[b][y] : weight;
+          weight = __shfl(weight, 16 * from + i);
+          const bool sees = pos < q_end[b] && (pos >= q_begin[b] || pos < sinks);
+#pragma unroll
+          for (int ch = 0; ch < NCB; ++ch)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int channel = 16 * ch + 4 * g + v;
+              float val;
+              if constexpr (Q8) val = __builtin_amdgcn_cvt_pk_f32_fp8(src[channel], false)[0] * scale;
+              else if constexpr (BF16) val = __uint_as_float((unsigned)((const uint16_t*)src)[channel] << 16);
+              else val = ((const float*)src)[channel];
+              if (sees && !(fabsf(val) < INFINITY)) o[b][ch][v] += weight * val;
+            }
+        }
+      }
+  };
+
+  auto work = [&](int t, int stage) __attribute__((always_inline)) {
+    const unsigned char* const k_lds = smem + stage * F::kTileBytes;
+    const unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
+    const int key0 = key0_of(t);
+    const bool masked = key0 + TN > w_end || (window && key0 < w_begin && key0 + TN > sinks);
+    const bool edge = is_edge(t);
+#pragma unroll
+    for (int nb = 0; nb < F::kBlocks; ++nb) {
+      const int block = wk * F::kBlocks + nb;
+      const unsigned char* const kb = k_lds + block * F::kBlock * F::kRowBytes;
+      const unsigned char* const vb = v_lds + block * F::kBlock * F::kRowBytes;
+      f32x4 s[RT][KT];
+#pragma unroll
+      for (int x = 0; x < KT; ++x) {
+        const int row = BF16 ? 16 * (i >> 2 & 1) + 8 * (i >> 3) + (i & 3) + 4 * x : i;
+        u32x4 kf[NSL];
+#pragma unroll
+        for (int sl = 0; sl < NSL; ++sl) kf[sl] = *(const u32x4*)(kb + row * F::kRowBytes + 16 * ((4 * sl + g) ^ F::k_flip(row)));
+#pragma unroll
+        for (int b = 0; b < RT; ++b) s[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int sl = 0; sl < NSL; ++sl)
+#pragma unroll
+          for (int b = 0; b < RT; ++b) {
+            if constexpr (BF16) {
+              s[b][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sl]),
+                                                                __builtin_bit_cast(bf16x8, qf[b][sl]), s[b][x], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[b][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sl][e]), __uint_as_float(qf[b][sl][e]),
+                                                               s[b][x], 0, 0, 0);
+            }
+          }
+      }
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int pos = key0 + block * F::kBlock + key_of(x, v);
+#pragma unroll
+            for (int b = 0; b < RT; ++b)
+              if (pos >= q_end[b] || (pos < q_begin[b] && pos >= sinks)) s[b][x][v] = -INFINITY;
+          }
+      }
+      // running maximum, moved only where it has grown by more than kRescaleThreshold
+      float mx[RT];
+      bool grow = false;
+#pragma unroll
+      for (int b = 0; b < RT; ++b) {
+        float m = s[b][0][0];
+#pragma unroll
+        for (int y = 1; y < 4 * KT; ++y) m = fmaxf(m, s[b][y / 4][y % 4]);
+        mx[b] = xor32_max(xor16_max(m));
+        grow |= (mx[b] - m_run[b]) * a.scale_log2e > kRescaleThreshold;
+      }
+      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+#pragma unroll
+        for (int b = 0; b < RT; ++b) {
+          const float m_new = fmaxf(m_run[b], mx[b]);
+          const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
+          m_run[b] = m_new;
+          l_run[b] *= alpha;
+#pragma unroll
+          for (int x = 0; x < NCB; ++x) o[b][x] *= alpha;
+        }
+      }
+      float w[RT][4 * KT];
+      u32x4 p[RT];
+#pragma unroll
+      for (int b = 0; b < RT; ++b) {
+        const float neg = -(m_run[b] * a.scale_log2e);
+#pragma unroll
+        for (int y = 0; y < 4 * KT; ++y) w[b][y] = __builtin_amdgcn_exp2f(fmaf(s[b][y / 4][y % 4], a.scale_log2e, neg));
+        if constexpr (BF16) {
+          // (weights are rounded to bf16 for the matrix cores; the sum adds the rounded ones)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const bf16x2 two = {(__bf16)w[b][2 * y], (__bf16)w[b][2 * y + 1]}, ones = {(__bf16)1.f, (__bf16)1.f};
+            l_run[b] = __builtin_amdgcn_fdot2_f32_bf16(two, ones, l_run[b], false);
+            p[b][y] = __builtin_bit_cast(unsigned, two);
+          }
+        } else {
+#pragma unroll
+          for (int y = 0; y < 4 * KT; ++y) l_run[b] += w[b][y];
+        }
+      }
+#pragma unroll
+      for (int ch = 0; ch < NCB; ++ch) {
+        if constexpr (BF16) {
+          typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+          const int row = 16 * (g & 1) + 8 * (g >> 1) + (i >> 2);
+          const unsigned char* const at = vb + row * F::kRowBytes + 16 * (2 * ch ^ F::v_flip(row)) + 8 * (i & 3);
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * F::kRowBytes));
+          const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int b = 0; b < RT; ++b)
+            o[b][ch] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, p[b]), o[b][ch], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int row = 4 * g + v;
+            const float val = *(const float*)(vb + row * F::kRowBytes + 16 * ((4 * ch + (i >> 2)) ^ F::v_flip(row)) + 4 * (i & 3));
+#pragma unroll
+            for (int b = 0; b < RT; ++b) o[b][ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(val, w[b][v], o[b][ch], 0, 0, 0);
+          }
+        }
+      }
+      if (edge) {
+        const unsigned rows = odd_rows[stage][block * F::kBlock / 32] >> (block * F::kBlock % 32);
+        const unsigned mine = __builtin_amdgcn_readfirstlane(BF16 ? rows : rows & 0xffffu);
+        if (mine) {
+#pragma unroll
+          for (int b = 0; b < RT; ++b)
+#pragma unroll
+            for (int y = 0; y < 4 * KT; ++y)
+              if constexpr (BF16) w[b][y] = (float)(__bf16)w[b][y];
+          add_odd(key0, block, mine, w);
+        }
+      }
+    }
+  };
+
+  // ---- the tiles
+  auto clear_odd = [&](int stage) {
+    if (tid < TN / 32) odd_rows[stage][tid] = 0;
+  };
+  if (t0 < t1) {
+    clear_odd(0);
+    if (F::kStages > 1) clear_odd(1);
+    ask_pages(t0);
+    ask_rows(t0);
+    ask_pages(t0 + 1);
+    __syncthreads();
+    store_rows(t0, 0);
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+      const int stage = F::kStages > 1 ? (t - t0) & 1 : 0;
+      if (t + 1 < t1) {
+        ask_rows(t + 1);
+        ask_pages(t + 2);
+      }
+      if (wave_row < n_rows) work(t, stage);  // (the others only carry their share of the tiles)
+      if constexpr (F::kStages > 1) {
+        // (the other stage was left before the last barrier; what is remembered of this tile's rows is cleared after
+        // the next one, two tiles before it is written again)
+        if (t + 1 < t1) store_rows(t + 1, stage ^ 1);
+        __syncthreads();
+        if (is_edge(t)) clear_odd(stage);
+        if (t + 2 < t1 && is_edge(t)) __syncthreads();
+      } else {
+        __syncthreads();
+        if (is_edge(t)) {
+          clear_odd(0);
+          __syncthreads();
+        }
+        if (t + 1 < t1) store_rows(t + 1, 0);
+        __syncthreads();
+      }
+    }
+  }
+
+  // ---- join the waves that have split the keys: a common maximum, then the sums
+#pragma unroll
+  for (int b = 0; b < RT; ++b) l_run[b] = xor32_sum(xor16_sum(l_run[b]));
+  if constexpr (F::WK > 1) {
+    f32x4* const part = (f32x4*)smem;                                     // [wave - 1][b][channel block][lane]
+    float* const stat = (float*)(smem + (F::WK - 1) * RT * NCB * 64 * 16);  // [wave - 1][b][2][lane]
+    __syncthreads();
+    if (wk > 0) {
+#pragma unroll
+      for (int b = 0; b < RT; ++b) {
+#pragma unroll
+        for (int ch = 0; ch < NCB; ++ch) part[(((wk - 1) * RT + b) * NCB + ch) * 64 + lane] = o[b][ch];
+        stat[(((wk - 1) * RT + b) * 2) * 64 + lane] = m_run[b];
+        stat[(((wk - 1) * RT + b) * 2 + 1) * 64 + lane] = l_run[b];
+      }
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int b = 0; b < RT; ++b) {
+      float top = m_run[b];
+#pragma unroll
+      for (int x = 0; x < F::WK - 1; ++x) top = fmaxf(top, stat[((x * RT + b) * 2) * 64 + lane]);
+      const float own = __builtin_amdgcn_exp2f((m_run[b] - top) * a.scale_log2e);
+      l_run[b] *= own;
+#pragma unroll
+      for (int ch = 0; ch < NCB; ++ch) o[b][ch] *= own;
+#pragma unroll
+      for (int x = 0; x < F::WK - 1; ++x) {
+        const float f = __builtin_amdgcn_exp2f((stat[((x * RT + b) * 2) * 64 + lane] - top) * a.scale_log2e);
+        l_run[b] += f * stat[((x * RT + b) * 2 + 1) * 64 + lane];
+#pragma unroll
+        for (int ch = 0; ch < NCB; ++ch) o[b][ch] += f * part[((x * RT + b) * NCB + ch) * 64 + lane];
+      }
+      m_run[b] = top;
+    }
+  }
+
+  // ---- write
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+    if (wave_row + 16 * b + i >= n_rows) continue;
+    const int r = q_row[b], t = r / a.group, head = kv * a.group + (r - t * a.group);
+    if (a.n_split > 1) {
+      const long long row = ((long long)unit * a.chunk.max_new * a.group + r) * a.n_split + split;
+      if (g == 0) {
+        a.stat[2 * row] = m_run[b];
+        a.stat[2 * row + 1] = l_run[b];
+      }
+#pragma unroll
+      for (int ch = 0; ch < NCB; ++ch) *(f32x4*)(a.part + row * D + 16 * ch + 4 * g) = o[b][ch];
+      continue;
+    }
+    const long long at = (long long)chunk_first(a.chunk, seq) + t;
+    if (at < 0 || at >= a.out.n_row) continue;
+    // a row that sees nothing, or keys of weight zero only, is zero
+    const float inv = l_run[b] == 0.f ? 0.f : 1.f / l_run[b];
+    unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
+#pragma unroll
+    for (int ch = 0; ch < NCB; ++ch) {
+      const f32x4 x = l_run[b] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[b][ch] * inv;
+      if constexpr (BF16) {
+        const bf16x2 lo2 = {(__bf16)x[0], (__bf16)x[1]}, hi2 = {(__bf16)x[2], (__bf16)x[3]};
+        *(uint2*)(dst + 32 * ch + 8 * g) = make_uint2(__builtin_bit_cast(unsigned, lo2), __builtin_bit_cast(unsigned, hi2));
+      } else {
+        *(f32x4*)(dst + 64 * ch + 16 * g) = x;
+      }
+    }
+  }
+}
+
+// Adds up what the workgroups of a row have left: a wave to a row, D / 64 channels to a lane.
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) void pages_join_kernel(AttendArgs a, int n_rows_all) {
+  constexpr int kPer = D / 64;
+  const int row = SCALEKV_WG_X * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= n_rows_all) return;
+  const int per_unit = a.chunk.max_new * a.group;
+  const int unit = row / per_unit, r = row - unit * per_unit, t = r / a.group;
+  const int seq = unit / a.c.n_kv_head, head = (unit - seq * a.c.n_kv_head) * a.group + (r - t * a.group);
+  if (t >= chunk_count(a.chunk, seq)) return;
+  const long long at = (long long)chunk_first(a.chunk, seq) + t;
+  if (at < 0 || at >= a.out.n_row) return;
+  const float* stat = a.stat + 2LL * row * a.n_split;
+  const float* part = a.part + (long long)row * a.n_split * D + kPer * lane;
+  float top = a.no_max;
+  for (int x = 0; x < a.n_split; ++x) top = fmaxf(top, stat[2 * x]);
+  float sum = 0.f, o[kPer] = {};
+  for (int x = 0; x < a.n_split; ++x) {
+    const float l = stat[2 * x + 1];
+    if (l == 0.f) continue;  // no keys there, or none of any weight
+    const float f = __builtin_amdgcn_exp2f((stat[2 * x] - top) * a.scale_log2e);
+    sum += f * l;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] += f * part[(long long)x * D + e];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    if constexpr (TYPE == kTypeBf16) ((__bf16*)dst)[kPer * lane + e] = (__bf16)(o[e] * inv);
+    else ((float*)dst)[kPer * lane + e] = o[e] * inv;
+  }
+}
+
+template <int TYPE, bool Q8, int D, int WQ, int RT>
+hipError_t launch_form(const AttendArgs& a, hipStream_t stream) {
+  using F = Form<TYPE, Q8, D, WQ, RT>;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_dynamic_lds((const void*)pages_attend_kernel<TYPE, Q8, D, WQ, RT>, F::kLds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((pages_attend_kernel<TYPE, Q8, D, WQ, RT>), dim3(a.n_wg), dim3(kThreads), F::kLds, stream, a);
+  return hipGetLastError();
+}
+
+template <int TYPE, bool Q8, int D>
+hipError_t launch_plan(const PagesPlan& plan, const AttendArgs& a, hipStream_t stream) {
+  if constexpr (TYPE == kTypeBf16) {
+    if (plan.row_waves == 4)
+      return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 4, 2>(a, stream) : launch_form<TYPE, Q8, D, 4, 1>(a, stream);
+    return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 1, 2>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);
+  } else {
+    return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4, 1>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);
+  }
+}
+
+}  // namespace
+
+PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& pages, int max_new, const MaskView& mask) {
+  constexpr int kComputeUnits = 256;
+  const int rows = max_new * (n_head / pages.n_kv_head);
+  PagesPlan p{};
+  if (dtype == kTypeF32) {
+    p.row_waves = rows <= 16 ? 1 : 4;
+    p.row_tiles = 1;
+  } else {
+    p.row_waves = rows <= 32 ? 1 : 4;
+    p.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
+  }
+  p.n_row_group = (rows + p.rows() - 1) / p.rows();
+  // keys that a row group can see at most
+  const long long cap = (long long)pages.width << pages.page_shift;
+  long long keys = cap;
+  if (mask.window > 0 && mask.causal) {
+    const long long seen = (long long)mask.n_sink + mask.window + max_new;
+    keys = seen < cap ? seen : cap;
+  }
+  const long long groups = (long long)n_seq * pages.n_kv_head * p.n_row_group;
+  long long split = 4 * kComputeUnits / groups;            // four workgroups to a compute unit
+  const long long most = keys / (p.row_waves == 1 ? 256 : 512);  // not worth a join below that
+  split = split < most ? split : most;
+  p.n_split = (int)(split < 1 ? 1 : split > 64 ? 64 : split);
+  return p;
+}
+
+hipError_t launch_pages_attend(int dtype, int d, int n_seq, int n_head, const PagesView& pages, const RowsView& q,
+                               const RowsView& out, const ChunkView& chunk, const MaskView& mask, float sm_scale,
+                               const PagesPlan& plan, void* ws, hipStream_t stream) {
+  AttendArgs a;
+  a.c = pages;
+  a.q = q;
+  a.out = out;
+  a.chunk = chunk;
+  a.mask = mask;
+  a.n_seq = n_seq;
+  a.group = n_head / pages.n_kv_head;
+  a.n_row_group = plan.n_row_group;
+  a.n_split = plan.n_split;
+  a.n_wg = n_seq * pages.n_kv_head * plan.n_row_group * plan.n_split;
+  a.scale_log2e = sm_scale * 1.4426950408889634f;
+  a.no_max = no_maximum(a.scale_log2e);
+  const int n_rows = n_seq * n_head * chunk.max_new;
+  a.part = (float*)ws;
+  a.stat = a.part + (size_t)n_rows * plan.n_split * d;
+  const bool q8 = pages.type == kTypeE4m3;
+  hipError_t e;
+  if (dtype == kTypeBf16) {
+    if (d == 128) e = q8 ? launch_plan<kTypeBf16, true, 128>(plan, a, stream) : launch_plan<kTypeBf16, false, 128>(plan, a, stream);
+    else e = q8 ? launch_plan<kTypeBf16, true, 64>(plan, a, stream) : launch_plan<kTypeBf16, false, 64>(plan, a, stream);
+  } else {
+    if (d == 128) e = q8 ? launch_plan<kTypeF32, true, 128>(plan, a, stream) : launch_plan<kTypeF32, false, 128>(plan, a, stream);
+    else e = q8 ? launch_plan<kTypeF32, true, 64>(plan, a, stream) : launch_plan<kTypeF32, false, 64>(plan, a, stream);
+  }
+  if (e != hipSuccess || plan.n_split == 1) return e;
+  const dim3 grid((n_rows + 3) / 4);
+  if (dtype == kTypeBf16) {
+    if (d == 128) hipLaunchKernelGGL((pages_join_kernel<kTypeBf16, 128>), grid, dim3(kThreads), 0, stream, a, n_rows);
+    else hipLaunchKernelGGL((pages_join_kernel<kTypeBf16, 64>), grid, dim3(kThreads), 0, stream, a, n_rows);
+  } else {
+    if (d == 128) hipLaunchKernelGGL((pages_join_kernel<kTypeF32, 128>), grid, dim3(kThreads), 0, stream, a, n_rows);
+    else hipLaunchKernelGGL((pages_join_kernel<kTypeF32, 64>), grid, dim3(kThreads), 0, stream, a, n_rows);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace scalekv

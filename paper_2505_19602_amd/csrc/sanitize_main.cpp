@@ -125,6 +125,35 @@ int main() {
     }
   EXPECT(scalekv_pyramid_budgets(4, 10, 11, win) == SCALEKV_ERR_INVALID_ARG);
   EXPECT(std::strlen(scalekv_version()) > 0);
+  // the paged cache: refused before a launch, and the host check of tables in buffers of exactly the documented size
+  {
+    scalekv_pages pg{fake(0x1000000), fake(0x2000000), nullptr, nullptr, 2 * 32 * 128, 32 * 128, 0, 0, 10, 2, 32, SCALEKV_BF16,
+                     (const int32_t*)fake(0x4000000), 3, (const int32_t*)fake(0x4100000)};
+    scalekv_rows rows{fake(0x5000000), 2 * 8 * 128, 8 * 128, 128, 8}, out_rows = rows;
+    scalekv_chunk chunk{8, nullptr, nullptr};
+    scalekv_mask mask{1, 0, 0};
+    size_t need = 1;
+    EXPECT(scalekv_pages_workspace_bytes(&s, &pg, 8, &mask, &need) == SCALEKV_OK);
+    EXPECT(scalekv_pages_workspace_bytes(&s, &pg, 0, &mask, &need) == SCALEKV_ERR_INVALID_ARG);
+    EXPECT(scalekv_pages_write(&s, &pg, &rows, nullptr, &chunk, nullptr) == SCALEKV_ERR_INVALID_ARG);
+    EXPECT(scalekv_pages_read(&s, &pg, nullptr, -1, &k, &v, nullptr) == SCALEKV_ERR_INVALID_ARG);
+    out_rows.ptr = fake(0x5000010);
+    EXPECT(scalekv_pages_attend(&s, &pg, &rows, &chunk, &mask, &out_rows, nullptr, 0, nullptr) == SCALEKV_ERR_INVALID_ARG);
+    scalekv_pages far = pg;
+    far.page_stride = (int64_t)1 << 40;
+    far.n_page = INT32_MAX;
+    EXPECT(scalekv_pages_write(&s, &far, &rows, &rows, &chunk, nullptr) == SCALEKV_ERR_UNSUPPORTED);
+    far = pg;
+    far.v = fake(0x1000000 + 128);
+    EXPECT(scalekv_pages_write(&s, &far, &rows, &rows, &chunk, nullptr) == SCALEKV_ERR_INVALID_ARG);
+    std::vector<int32_t> table{4, 5, 6}, len{90}, count{8}, first{0};
+    EXPECT(scalekv_pages_check(&s, &pg, table.data(), len.data(), &chunk, first.data(), count.data(), 8) == SCALEKV_OK);
+    count[0] = 9;
+    EXPECT(scalekv_pages_check(&s, &pg, table.data(), len.data(), &chunk, first.data(), count.data(), 8) == SCALEKV_ERR_INVALID_ARG);
+    table[2] = 10;
+    EXPECT(scalekv_pages_check(&s, &pg, table.data(), len.data(), nullptr, nullptr, nullptr, 0) == SCALEKV_ERR_INVALID_ARG);
+  }
+
   std::printf("ABI host sanitizer run complete, %d failed expectations\n", failures);
   return failures != 0;
 }

@@ -1,0 +1,264 @@
+"""Host-only checks of the paged cache's entry points: what they refuse (pointers below are fake but aligned and never
+dereferenced: every call is refused before a launch), the host check of tables, and the 64-bit definitions that the GPU
+tests compare with.  No GPU needed."""
+import ctypes
+import math
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_19602_amd as skv
+import pages_util as P
+from paper_2505_19602_amd import binding as B
+from paper_2505_19602_amd import build as hip_build
+
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+F32, BF16, E4M3 = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(skv.lib_path()):
+        hip_build.build(force=True)
+    return skv.lib()
+
+
+def _err(L):
+    return L.scalekv_last_error().decode()
+
+
+def _shape(**kw):
+    base = dict(n_seq=2, n_head=4, head_dim=128, dtype=BF16, sm_scale=0.0)
+    base.update(kw)
+    return B._CShape(*base.values())
+
+
+def _pages(**kw):
+    """Ten pages of 32 rows, two KV heads, of 128 elements: 16 KB a page in 16 bits."""
+    d, heads, rows = 128, 2, 32
+    base = dict(k=0x1000000, v=0x2000000, k_scale=0x3000000, v_scale=0x3100000, page_stride=heads * rows * d,
+                head_stride=rows * d, scale_page_stride=heads * rows, scale_head_stride=rows, n_page=10, n_kv_head=heads,
+                page_rows=rows, dtype=BF16, table=0x4000000, table_width=5, len=0x4100000)
+    base.update(kw)
+    return B._CPages(*base.values())
+
+
+def _rows(**kw):
+    base = dict(ptr=0x5000000, seq_stride=4 * 8 * 128, head_stride=8 * 128, row_stride=128, n_row=8)
+    base.update(kw)
+    return B._CRows(*base.values())
+
+
+def _chunk(**kw):
+    base = dict(max_new=8, first=0, count=0)
+    base.update(kw)
+    return B._CChunk(*base.values())
+
+
+def _mask(causal=1, window=0, n_sink=0):
+    return B._CMask(causal, window, n_sink)
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+BAD_SHAPES = [(dict(n_seq=0), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(dtype=E4M3), UNSUPPORTED),
+              (dict(n_seq=70000), UNSUPPORTED), (dict(sm_scale=math.nan), INVALID)]
+BAD_SIZES = [(dict(dtype=7), UNSUPPORTED, "dtype"), (dict(dtype=F32), UNSUPPORTED, "neither the shape's"),
+             (dict(page_rows=24), UNSUPPORTED, "power of two"), (dict(page_rows=8), UNSUPPORTED, "page_rows"),
+             (dict(page_rows=512), UNSUPPORTED, "page_rows"), (dict(page_rows=0), UNSUPPORTED, "page_rows"),
+             (dict(page_rows=-32), UNSUPPORTED, "page_rows"), (dict(n_page=0), INVALID, "n_page"),
+             (dict(n_kv_head=3), INVALID, "divide"), (dict(n_kv_head=0), INVALID, "n_kv_head"),
+             (dict(n_kv_head=8), INVALID, "divide"), (dict(table_width=0), INVALID, "table_width"),
+             (dict(table_width=1 << 26), UNSUPPORTED, "2^30")]
+BAD_PAGES = BAD_SIZES + [
+    (dict(k=0), INVALID, "pages.k"), (dict(v=0), INVALID, "pages.v"), (dict(k=0x1000008), INVALID, "aligned"),
+    (dict(head_stride=32 * 128 - 8), INVALID, "head_stride"), (dict(head_stride=32 * 128 + 4), INVALID, "multiple"),
+    (dict(page_stride=2 * 32 * 128 - 8), INVALID, "page_stride"), (dict(page_stride=1 << 41), INVALID, "page_stride"),
+    (dict(page_stride=1 << 40, n_page=1 << 20), UNSUPPORTED, "too far"),
+    (dict(dtype=E4M3, k_scale=0), INVALID, "scale"), (dict(dtype=E4M3, scale_head_stride=31), INVALID, "scale_head_stride"),
+    (dict(dtype=E4M3, scale_page_stride=63), INVALID, "scale_page_stride"),
+    (dict(table=0), INVALID, "table"), (dict(len=0), INVALID, "len")]
+BAD_CHUNKS = [(dict(max_new=0), INVALID, "max_new"), (dict(max_new=-1), INVALID, "max_new"),
+              (dict(max_new=9), INVALID, "n_row"), (dict(max_new=1 << 27), UNSUPPORTED, "too large")]
+BAD_ROWS = [(dict(ptr=0), INVALID, "ptr"), (dict(ptr=0x5000004), INVALID, "aligned"), (dict(row_stride=-128), INVALID, "stride"),
+            (dict(head_stride=100), INVALID, "stride"), (dict(seq_stride=1 << 41), INVALID, "stride"),
+            (dict(n_row=-1), INVALID, "n_row"), (dict(n_row=7), INVALID, "n_row"),
+            (dict(n_row=2 ** 31 - 1, row_stride=1 << 39), UNSUPPORTED, "too far")]
+
+
+def _write(L, shape=None, pages=None, k=None, v=None, chunk=None):
+    return L.scalekv_pages_write(_ref(shape or _shape()), _ref(pages or _pages()), _ref(k or _rows()),
+                                 _ref(v or _rows(ptr=0x6000000)), _ref(chunk or _chunk()), None)
+
+
+def _read(L, shape=None, pages=None, n_row=8, k=None, v=None):
+    kv = lambda at: B._CKv(at, 4 * 10 * 128, 10 * 128, 10)
+    return L.scalekv_pages_read(_ref(shape or _shape()), _ref(pages or _pages()), None, n_row, _ref(k or kv(0x5000000)),
+                                _ref(v or kv(0x6000000)), None)
+
+
+def _attend(L, shape=None, pages=None, q=None, chunk=None, mask=None, out=None, ws=None, ws_bytes=0):
+    return L.scalekv_pages_attend(_ref(shape or _shape()), _ref(pages or _pages()), _ref(q or _rows()),
+                                  _ref(chunk or _chunk()), _ref(mask or _mask()), _ref(out or _rows(ptr=0x6000000)),
+                                  ctypes.c_void_p(ws), ctypes.c_size_t(ws_bytes), None)
+
+
+def _need(L, shape=None, pages=None, max_new=8, mask=None):
+    out = ctypes.c_size_t(77)
+    st = L.scalekv_pages_workspace_bytes(_ref(shape or _shape()), _ref(pages or _pages()), max_new, _ref(mask or _mask()),
+                                         ctypes.byref(out))
+    return st, out.value
+
+
+def test_shapes_pages_and_chunks_that_are_refused(L):
+    for kw, status in BAD_SHAPES:
+        s = _shape(**kw)
+        assert _write(L, s) == _read(L, s) == _attend(L, s) == _need(L, s)[0] == status, kw
+    for kw, status, word in BAD_PAGES:
+        for call in (_write, _read, _attend):
+            assert call(L, pages=_pages(**kw)) == status, (call, kw)
+            assert word in _err(L), (kw, _err(L))
+    for kw, status, word in BAD_SIZES:
+        assert _need(L, pages=_pages(**kw))[0] == status and word in _err(L), kw
+    for kw, status, word in BAD_CHUNKS:
+        for call in (_write, _attend):
+            assert call(L, chunk=_chunk(**kw)) == status and word in _err(L), (call, kw, _err(L))
+    for kw, status, word in BAD_ROWS:
+        bad = _rows(**kw)
+        for got in (_write(L, k=bad), _write(L, v=bad), _attend(L, q=bad), _attend(L, out=bad)):
+            assert got == status and word in _err(L), (kw, _err(L))
+    for f, n in ((L.scalekv_pages_write, 6), (L.scalekv_pages_read, 7), (L.scalekv_pages_attend, 9)):
+        assert f(None, *([None] * (n - 1))) == INVALID
+        assert f(ctypes.byref(_shape()), *([None] * (n - 1))) == INVALID and "pages is NULL" in _err(L)
+    assert L.scalekv_pages_workspace_bytes(ctypes.byref(_shape()), ctypes.byref(_pages()), 1, None, None) == INVALID
+    assert _need(L, max_new=0)[0] == INVALID
+
+
+def test_masks_workspaces_and_overlaps_that_are_refused(L):
+    for mask, word in ((_mask(causal=2), "causal"), (_mask(window=-1), "window"), (_mask(n_sink=-1), "n_sink")):
+        assert _attend(L, mask=mask) == INVALID and word in _err(L)
+        assert _need(L, mask=mask)[0] == INVALID
+    # a single token of two sequences over a long table needs a workspace
+    long, one = _pages(table_width=4000), _chunk(max_new=1)
+    st, need = _need(L, pages=long, max_new=1)
+    assert st == OK and need > 0
+    assert _attend(L, pages=long, chunk=one) == WORKSPACE and "needed" in _err(L)
+    assert _attend(L, pages=long, chunk=one, ws=0x7000000, ws_bytes=need - 1) == WORKSPACE
+    assert _attend(L, pages=long, chunk=one, ws=0x7000008, ws_bytes=need) == INVALID and "aligned" in _err(L)
+    for at in (0x1000000, 0x2000000, 0x5000000, 0x6000000):
+        assert _attend(L, pages=long, chunk=one, ws=at, ws_bytes=need) == INVALID and "workspace overlaps" in _err(L)
+    # rows of out that coincide, out on q but not exactly, out and new rows in the pool
+    for kw in (dict(head_stride=0), dict(row_stride=0), dict(seq_stride=0)):
+        assert _attend(L, out=_rows(ptr=0x6000000, **kw)) == INVALID and "coincide" in _err(L)
+    assert _attend(L, out=_rows(ptr=0x5000000 + 256)) == INVALID and "overlaps q" in _err(L)
+    assert _attend(L, out=_rows(row_stride=256)) == INVALID and "overlaps q" in _err(L)
+    for at in (0x1000000, 0x2000000 + 9 * 16384):
+        assert _attend(L, out=_rows(ptr=at)) == INVALID and "overlaps the pool" in _err(L)
+        assert _write(L, k=_rows(ptr=at)) == _write(L, v=_rows(ptr=at)) == INVALID and "overlaps the pool" in _err(L)
+        assert _read(L, k=B._CKv(at, 4 * 1280, 1280, 10)) == INVALID and "overlaps the pool" in _err(L)
+    q8 = _pages(dtype=E4M3)
+    assert _attend(L, pages=q8, out=_rows(ptr=0x3000000)) == INVALID
+    assert _read(L, v=B._CKv(0x5000000, 4 * 1280, 1280, 10)) == INVALID and "overlap" in _err(L)
+    assert _read(L, n_row=11) == INVALID and "capacity" in _err(L)
+    assert _read(L, n_row=-1) == INVALID
+    assert _read(L, n_row=0) == OK                                   # nothing to do needs no device
+
+
+def test_keys_and_values_that_share_bytes_are_refused(L):
+    # keys and values page by page in turn are fine, a few bytes off they are not (no call here gets as far as a launch)
+    bytes_of_page = 2 * 32 * 128 * 2
+    for gap in (0, 256, -256, 32 * 128 * 2 - 16, bytes_of_page, -bytes_of_page, 9 * bytes_of_page, 32 * 128 * 2,
+                -32 * 128 * 2, 10 * bytes_of_page - 16):
+        assert _write(L, pages=_pages(v=0x1000000 + gap)) == INVALID, gap
+        assert "pages.k and pages.v overlap" in _err(L)
+    apart = 2 * bytes_of_page // 2                                    # k pages, v pages in turn
+    for gap in (16, 32 * 128 * 2 - 16, -16):
+        assert _write(L, pages=_pages(page_stride=2 * 2 * 32 * 128, v=0x1000000 + gap)) == INVALID
+    assert _write(L, pages=_pages(page_stride=2 * 2 * 32 * 128, v=0x1000000 + apart + 16)) == INVALID
+    assert _write(L, pages=_pages(dtype=E4M3, v_scale=0x3000000 + 40)) == INVALID and "v_scale overlap" in _err(L)
+    assert _write(L, pages=_pages(dtype=E4M3, k_scale=0x1000000)) == INVALID and "scales overlap" in _err(L)
+
+
+def test_the_workspace_covers_every_size_and_is_not_asked_for_where_rows_abound(L):
+    for n_seq, heads, kv, width, new in ((1, 8, 1, 4096, 1), (2, 32, 8, 4096, 1), (1, 1, 1, 1, 1), (64, 32, 8, 125, 1)):
+        st, need = _need(L, _shape(n_seq=n_seq, n_head=heads), _pages(n_kv_head=kv, table_width=width), new)
+        assert st == OK and need % 4 == 0 and need <= 64 * n_seq * heads * new * 130 * 4
+    assert _need(L, _shape(n_seq=16, n_head=16), _pages(n_kv_head=16, table_width=200), 4096) == (OK, 0)
+
+
+def _check(L, table, lens, count=None, first=None, max_new=None, n_row=0, **kw):
+    width = len(table[0])
+    ints = lambda x: None if x is None else (ctypes.c_int32 * len(x))(*x)
+    chunk = None if max_new is None else ctypes.byref(_chunk(max_new=max_new))
+    return L.scalekv_pages_check(ctypes.byref(_shape(n_seq=len(table))), ctypes.byref(_pages(table_width=width, **kw)),
+                                 ints([x for r in table for x in r]), ints(lens), chunk, ints(first), ints(count), n_row)
+
+
+def test_tables_with_mistakes_are_named(L):
+    good = [[0, 1, -1], [2, 9, 5]]
+    assert _check(L, good, [40, 96]) == OK                           # (entries behind the last page are not used)
+    assert _check(L, good, [40, 96], count=[8, 0], max_new=8, n_row=8) == OK
+    assert _check(L, good, [0, 0]) == OK
+    for table, lens, kw, word in (
+            (good, [65, 96], {}, "table[0][2]"), ([[0, 10, 1], [2, 3, 4]], [40, 40], {}, "table[0][1] = 10"),
+            ([[0, -7, 1], [2, 3, 4]], [40, 40], {}, "table[0][1] = -7"), (good, [-1, 5], {}, "len[0]"),
+            (good, [40, 97], {}, "len[1]"), (good, [40, 96], dict(max_new=8, count=[9, 0], n_row=8), "count[0]"),
+            (good, [40, 96], dict(max_new=8, count=[-1, 0], n_row=8), "count[0]"),
+            (good, [40, 3], dict(max_new=8, n_row=8), "count[1]"), (good, [40, 96], dict(max_new=8, n_row=7), "sequence 0"),
+            (good, [40, 96], dict(max_new=8, first=[0, 5], n_row=8), "sequence 1"),
+            (good, [40, 96], dict(max_new=8, first=[-1, 0], n_row=8), "sequence 0")):
+        assert _check(L, table, lens, **kw) == INVALID and word in _err(L), (kw, _err(L))
+    # a shared prefix is fine until somebody writes to it
+    shared = [[0, 1, 2], [0, 1, 3]]
+    assert _check(L, shared, [70, 80]) == OK
+    assert _check(L, shared, [70, 80], count=[6, 16], max_new=16, n_row=16) == OK
+    assert _check(L, shared, [70, 80], count=[7, 16], max_new=16, n_row=16) == INVALID and "page 1" in _err(L)
+    assert _check(L, [[0, 1, 0], [2, 3, 4]], [70, 80], count=[1, 0], max_new=1, n_row=1) == INVALID and "page 0" in _err(L)
+    assert L.scalekv_pages_check(ctypes.byref(_shape()), ctypes.byref(_pages()), None, None, None, None, None, 0) == INVALID
+
+
+def test_the_binding_refuses_tensors_that_are_not_what_it_says():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    table, lens = torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    for args in ((k.half(), k.half(), table, lens), (k, k.float(), table, lens), (k, k[:2], table, lens), (k, k, table, lens)):
+        with pytest.raises(skv.ScaleKVError):                         # (the last: not on a device)
+            skv.Pages(*args)
+
+
+# ---- the definitions in 64 bits that the GPU tests use
+
+def test_codes_are_the_nearest_e4m3_values_ties_to_even():
+    values = sorted({float(v) for v in torch.arange(256, dtype=torch.uint8).view(P.E4M3).float() if math.isfinite(v)})
+    assert len(values) == 253 and values[-1] == 448.0 and min(v for v in values if v > 0) == 2.0 ** -9
+    even = {float(v) for v in torch.arange(0, 256, 2, dtype=torch.uint8).view(P.E4M3).float()}
+    for a, b in zip(values, values[1:]):
+        for x, want in ((a, a), (a + 0.25 * (b - a), a), (a + 0.75 * (b - a), b), ((a + b) / 2, a if a in even else b)):
+            assert P.nearest_code(x) == want
+    x = torch.randn(50, 64, generator=torch.Generator().manual_seed(1)) * 2.0 ** torch.randint(-40, 40, (50, 1)).float()
+    x[3] = 0
+    x[4, 7], x[5, 8] = math.inf, math.nan
+    codes, scale = P.quantised_tensor(x)
+    for i in range(50):
+        row, k = P.quantised(x[i].double().numpy())
+        assert int(scale[i]) == k + 127 and np.array_equal(codes[i].float().numpy(), row, equal_nan=True)
+        fine = torch.isfinite(x[i])
+        err = (x[i].double().numpy() - np.ldexp(row, k))[fine]
+        assert np.all(np.abs(err) <= np.maximum(2.0 ** -4 * np.abs(x[i].double().numpy()[fine]), 2.0 ** (k - 10)))
+
+
+def test_the_64_bit_attention_is_a_softmax_over_what_a_token_sees():
+    cache = P.Cache(1, [50], 1, 64, 16, torch.float32, torch.float32)
+    q = torch.randn(2, 9, 64, generator=torch.Generator().manual_seed(3))
+    k, v = cache.rows("k", 0)[0], cache.rows("v", 0)[0]
+    for causal, window, sinks in ((False, 0, 0), (True, 0, 0), (True, 5, 2), (False, 5, 0)):
+        hidden = torch.stack([~P.sees(41 + t, 50, causal, window, sinks) for t in range(9)])
+        want = torch.softmax((q.double() @ k.t() / 8).masked_fill(hidden, -math.inf), -1) @ v
+        out, tol = P.attend(cache, 0, q, causal, window, sinks, 0.125)
+        assert torch.allclose(out, want, atol=1e-12) and torch.all(tol > 0) and float(tol.max()) < 1e-2
+    assert P.sees(0, 4, True, 1, 0).tolist() == [True, False, False, False]
+    assert P.sees(3, 5, True, 2, 1).tolist() == [True, False, True, True, False]
+    assert not P.sees(-2, 5, True, 0, 3).any()
