@@ -81,7 +81,8 @@ _fast = None      # the _marshal module, bound to the loaded library's entry poi
 
 # entry points in the order of struct Entry in csrc/marshal.cpp
 _MARSHALLED = ("scalekv_step", "scalekv_step_static", "scalekv_step_append_first", "scalekv_score", "scalekv_select",
-               "scalekv_select_window", "scalekv_select_positional", "scalekv_compact", "scalekv_attend", "scalekv_asi")
+               "scalekv_select_window", "scalekv_select_positional", "scalekv_compact", "scalekv_attend", "scalekv_asi",
+               "scalekv_pages_write", "scalekv_pages_read", "scalekv_pages_attend")
 
 
 def lib_path() -> str:
@@ -610,7 +611,7 @@ class Pages:
     lengths are read when a call's kernels run: they may be changed between calls, and between replays of a captured call.
     """
 
-    __slots__ = ("k", "v", "table", "lens", "k_scale", "v_scale", "c")
+    __slots__ = ("k", "v", "table", "lens", "k_scale", "v_scale", "c", "_native")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
@@ -642,6 +643,7 @@ class Pages:
         self.c = _CPages(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(),
                          0 if v_scale is None else v_scale.data_ptr(), *strides[0], *scale_strides[0], n_page, heads, rows,
                          _CACHE_DTYPES[k.dtype], table.data_ptr(), table.shape[1], lens.data_ptr())
+        self._native = (ctypes.addressof(self.c), table.shape[0], d, k.device.index)   # for csrc/marshal.cpp
 
     @staticmethod
     def _strides(t, unit, sizes, name):
@@ -696,6 +698,10 @@ def pages_write(shape: Shape, pages: Pages, k_new: torch.Tensor, v_new: torch.Te
                 first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
                 max_new: Optional[int] = None) -> None:
     """scalekv_pages_write: rows of new tokens, [S, KV heads, n, d] or packed [N, KV heads, d], into their pages."""
+    r = _marshaller().pages_write(shape, pages, k_new, v_new, first, count, max_new)
+    if r is not None:
+        _checked(r)
+        return
     _pages_of(shape, pages)
     heads = pages.k.shape[1]
     k, v = _rows(k_new, shape, heads, "k_new"), _rows(v_new, shape, heads, "v_new")
@@ -709,6 +715,10 @@ def pages_write(shape: Shape, pages: Pages, k_new: torch.Tensor, v_new: torch.Te
 def pages_read(shape: Shape, pages: Pages, idx: Optional[torch.Tensor], n_row: int, k_dst: torch.Tensor,
                v_dst: torch.Tensor) -> None:
     """scalekv_pages_read: rows [0, n_row), or those that idx [S,H,n_row] int32 lists, into caches [S,H,capacity,d]."""
+    r = _marshaller().pages_read(shape, pages, idx, n_row, k_dst, v_dst)
+    if r is not None:
+        _checked(r)
+        return
     _pages_of(shape, pages)
     n_row = index(n_row)
     _idx_tensor(idx, shape, n_row, "idx")
@@ -734,6 +744,10 @@ def pages_attend(shape: Shape, pages: Pages, q: torch.Tensor, out: torch.Tensor,
     """scalekv_pages_attend: q, out [S,H,n,d] or packed [N,H,d]; the new tokens attend over the rows of their sequences,
     themselves included.  causal: up to a token's own position; window: only the last `window` of those, and the
     first n_sink rows of the cache."""
+    r = _marshaller().pages_attend(shape, pages, q, out, ws, causal, window, n_sink, first, count, max_new)
+    if r is not None:
+        _checked(r)
+        return
     _pages_of(shape, pages)
     cq, co = _rows(q, shape, shape.n_head, "q"), _rows(out, shape, shape.n_head, "out")
     if q.dim() != out.dim():

@@ -15,6 +15,7 @@
 #include <Python.h>
 
 #include <ATen/core/TensorBase.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -37,10 +38,13 @@ struct Entry {
   decltype(&scalekv_compact) compact;
   decltype(&scalekv_attend) attend;
   decltype(&scalekv_asi) asi;
+  decltype(&scalekv_pages_write) pages_write;
+  decltype(&scalekv_pages_read) pages_read;
+  decltype(&scalekv_pages_attend) pages_attend;
 } g_entry;
 bool g_bound = false;
 
-PyObject *g_n_seq, *g_n_head, *g_head_dim, *g_dtype, *g_sm_scale;  // interned attribute names
+PyObject *g_n_seq, *g_n_head, *g_head_dim, *g_dtype, *g_sm_scale, *g_native;  // interned attribute names
 
 struct Shape {
   scalekv_shape c;
@@ -391,6 +395,116 @@ PyObject* py_asi(PyObject*, PyObject* const* a, Py_ssize_t n) {
                 0);
 }
 
+// ---- the paged cache.  binding.Pages has checked its tensors; its attribute _native is a tuple of
+// (address of its scalekv_pages, n_seq, head_dim, device).
+struct PagesArg {
+  const scalekv_pages* c;
+  long device;
+};
+
+bool to_pages(PyObject* o, const Shape& s, PagesArg* p) {
+  PyObject* t = PyObject_GetAttr(o, g_native);
+  if (!t) { PyErr_Clear(); return false; }
+  bool ok = PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 4;
+  if (ok) {
+    p->c = static_cast<const scalekv_pages*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(t, 0)));  // (owned by the object itself)
+    p->device = PyLong_AsLong(PyTuple_GET_ITEM(t, 3));
+    ok = p->c && PyLong_AsLong(PyTuple_GET_ITEM(t, 1)) == s.c.n_seq && PyLong_AsLong(PyTuple_GET_ITEM(t, 2)) == s.c.head_dim;
+  }
+  Py_DECREF(t);
+  if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+  return ok && p->device == c10::hip::current_device();
+}
+
+// [S, heads, n, d] or packed [N, heads, d]; *dims: 0 takes the tensor's own, which another tensor then has to match
+bool token_rows(PyObject* o, const Shape& s, int32_t heads, long device, int64_t* dims, scalekv_rows* r) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::TensorBase& t = THPVariable_Unpack(o);
+  const int64_t n = t.dim();
+  if ((n != 4 && n != 3) || (*dims && n != *dims) || t.scalar_type() != s.type || !t.is_cuda() ||
+      t.device().index() != device || t.size(n - 1) != s.c.head_dim || t.stride(n - 1) != 1 ||
+      t.size(1) != heads || (n == 4 && t.size(0) != s.c.n_seq))
+    return false;
+  *dims = n;
+  const int64_t row = n == 4 ? 2 : 0;
+  if (t.size(row) > INT32_MAX) return false;
+  auto stride = [&](int64_t d) { return t.size(d) == 1 ? 0 : t.stride(d); };  // a dimension of one has none of its own
+  *r = scalekv_rows{t.data_ptr(), n == 4 ? stride(0) : 0, stride(1), stride(row), (int32_t)t.size(row)};
+  return true;
+}
+
+// (first, count, max_new) behind `rows`, a tensor of `dims` dimensions
+bool to_chunk(PyObject* const* a, const Shape& s, long device, int64_t dims, const scalekv_rows& rows, scalekv_chunk* c) {
+  const int32_t** to[2] = {&c->first, &c->count};
+  for (int i = 0; i < 2; ++i) {
+    *to[i] = nullptr;
+    if (a[i] == Py_None) continue;
+    if (!THPVariable_CheckExact(a[i])) return false;
+    const at::TensorBase& t = THPVariable_Unpack(a[i]);
+    if (t.dim() != 1 || t.size(0) != s.c.n_seq || t.scalar_type() != at::kInt || !t.is_contiguous() || !t.is_cuda() ||
+        t.device().index() != device)
+      return false;
+    *to[i] = static_cast<const int32_t*>(t.data_ptr());
+  }
+  if (dims == 3 && s.c.n_seq > 1 && (a[0] == Py_None || a[2] == Py_None)) return false;
+  c->max_new = rows.n_row;
+  return a[2] == Py_None || to_int(a[2], &c->max_new);
+}
+
+// (shape, pages, k_new, v_new, first, count, max_new)
+PyObject* py_pages_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  SCALEKV_ARITY(7);
+  Shape s;
+  PagesArg p;
+  scalekv_rows k, v;
+  scalekv_chunk chunk;
+  int64_t dims = 0;
+  if (!to_shape(a[0], &s) || !to_pages(a[1], s, &p) || !token_rows(a[2], s, p.c->n_kv_head, p.device, &dims, &k) ||
+      !token_rows(a[3], s, p.c->n_kv_head, p.device, &dims, &v) || !to_chunk(a + 4, s, p.device, dims, k, &chunk))
+    return none();
+  void* const stream = current_stream();
+  return answer(unlocked([&] { return g_entry.pages_write(&s.c, p.c, &k, &v, &chunk, stream); }), 0);
+}
+
+// (shape, pages, idx, n_row, k_dst, v_dst)
+PyObject* py_pages_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  SCALEKV_ARITY(6);
+  Shape s;
+  PagesArg p;
+  int32_t rows;
+  int32_t* idx;
+  scalekv_kv k, v;
+  if (!to_shape(a[0], &s) || !to_pages(a[1], s, &p) || !to_int(a[3], &rows) || !optional_plane(a[2], s, rows, &idx) ||
+      !cache(a[4], s, &k) || !cache(a[5], s, &v))
+    return none();
+  for (PyObject* o : {a[2], a[4], a[5]})
+    if (o != Py_None && THPVariable_Unpack(o).device().index() != p.device) return none();
+  void* const stream = current_stream();
+  return answer(unlocked([&] { return g_entry.pages_read(&s.c, p.c, idx, rows, &k, &v, stream); }), 0);
+}
+
+// (shape, pages, q, out, ws, causal, window, n_sink, first, count, max_new)
+PyObject* py_pages_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  SCALEKV_ARITY(11);
+  Shape s;
+  PagesArg p;
+  scalekv_rows q, out;
+  scalekv_chunk chunk;
+  scalekv_mask mask;
+  void* ws;
+  size_t bytes;
+  int64_t dims = 0;
+  if (!to_shape(a[0], &s) || !to_pages(a[1], s, &p) || !token_rows(a[2], s, s.c.n_head, p.device, &dims, &q) ||
+      !token_rows(a[3], s, s.c.n_head, p.device, &dims, &out) || !workspace(a[4], &ws, &bytes) || !PyBool_Check(a[5]) ||
+      !to_int(a[6], &mask.window) || !to_int(a[7], &mask.n_sink) || !to_chunk(a + 8, s, p.device, dims, q, &chunk))
+    return none();
+  if (bytes && THPVariable_Unpack(a[4]).device().index() != p.device) return none();
+  mask.causal = a[5] == Py_True;
+  void* const stream = current_stream();
+  return answer(
+      unlocked([&] { return g_entry.pages_attend(&s.c, p.c, &q, &chunk, &mask, &out, ws, bytes, stream); }), 0);
+}
+
 // ---- a call whose arguments are marshalled once: prepared(stream or None) -> as the call itself
 struct Prepared {
   PyObject_HEAD
@@ -467,7 +581,8 @@ PyMethodDef g_methods[] = {
     SCALEKV_METHOD(bind), SCALEKV_METHOD(step), SCALEKV_METHOD(step_static), SCALEKV_METHOD(append_first),
     SCALEKV_METHOD(score), SCALEKV_METHOD(select), SCALEKV_METHOD(select_window), SCALEKV_METHOD(select_positional),
     SCALEKV_METHOD(compact), SCALEKV_METHOD(attend), SCALEKV_METHOD(asi), SCALEKV_METHOD(prepare_step),
-    SCALEKV_METHOD(prepare_append_first), {nullptr, nullptr, 0, nullptr}};
+    SCALEKV_METHOD(prepare_append_first), SCALEKV_METHOD(pages_write), SCALEKV_METHOD(pages_read),
+    SCALEKV_METHOD(pages_attend), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods};
 
 }  // namespace
@@ -478,6 +593,7 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   g_head_dim = PyUnicode_InternFromString("head_dim");
   g_dtype = PyUnicode_InternFromString("dtype");
   g_sm_scale = PyUnicode_InternFromString("sm_scale");
+  g_native = PyUnicode_InternFromString("_native");
   g_prepared_type.tp_name = "_marshal.Prepared";
   g_prepared_type.tp_basicsize = sizeof(Prepared);
   g_prepared_type.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL;
