@@ -22,16 +22,10 @@
 // Masked keys.  A weight of zero does not hide a value that is infinite or NaN from the product.  Rows hidden from all rows
 // of the workgroup are zeros in LDS; in the few tiles that some of its rows see and others do not (`edge`), values that
 // are not finite are taken out of the tile, remembered, and added for the rows that do see them (`add_odd`).
-#include "pages.h"
+#include "pages_attend.h"
 
 namespace scalekv {
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 constexpr int kThreads = 256;
 
@@ -56,64 +50,10 @@ struct Form {
   static constexpr int kRows = 16 * RT * WQ;             // query rows of a workgroup
   static constexpr int kJoinBytes = WK > 1 ? (WK - 1) * 64 * RT * (kChans * 16 + 8) : 0;
   static constexpr int kLds = 2 * kStages * kTileBytes > kJoinBytes ? 2 * kStages * kTileBytes : kJoinBytes;
-  // chunk c of row r sits in slot c ^ k_flip(r) of a K row, c ^ v_flip(r) of a V row
-  __device__ static constexpr int k_flip(int r) {
-    if (!kBf16) return r & 15;
-    const int high = (r >> 4 & 1) | (r >> 3 & 1) << 1;
-    return D == 128 ? (r & 3) | high << 2 : (r >> 1 & 1) | high << 1;
-  }
-  __device__ static constexpr int v_flip(int r) {
-    if (!kBf16) return r & 15;
-    return D == 128 ? (r & 3) << 1 | (r >> 4 & 1) << 3 : (r >> 1 & 1) << 1 | (r >> 4 & 1) << 2;
-  }
+  static_assert(4 * 16 * RT * D * 4 <= kLds, "the sums of all waves fit (add_odd)");
+  __device__ static constexpr int k_flip(int r) { return kBf16 ? k_flip_bf16<D>(r) : r & 15; }
+  __device__ static constexpr int v_flip(int r) { return kBf16 ? v_flip_bf16<D>(r) : r & 15; }
 };
-
-struct AttendArgs {
-  PagesView c;
-  RowsView q, out;
-  ChunkView chunk;
-  MaskView mask;
-  int n_seq, group, n_row_group, n_split, n_wg;
-  float scale_log2e, no_max;
-  float *part, *stat;  // partial sums [row][split][D], their {maximum, sum} [row][split][2]
-};
-
-// sixteen codes of a row with its scale, as the products take them
-__device__ __forceinline__ void widen(const u32x4& x, float s, u32x4 (&y)[2]) {  // bf16
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i / 2][i % 2 * 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], s, false));
-    y[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], s, true));
-  }
-}
-__device__ __forceinline__ void widen(const u32x4& x, float s, u32x4 (&y)[4]) {  // fp32
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], true);
-    y[i][0] = __float_as_uint(lo[0] * s);
-    y[i][1] = __float_as_uint(lo[1] * s);
-    y[i][2] = __float_as_uint(hi[0] * s);
-    y[i][3] = __float_as_uint(hi[1] * s);
-  }
-}
-// zeros in the place of what is not finite; whether there was any
-template <bool BF16>
-__device__ __forceinline__ bool take_odd(u32x4& x) {
-  bool odd = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (BF16) {
-      const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
-      odd |= lo || hi;
-      x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-    } else {
-      const bool it = (x[i] & 0x7f800000u) == 0x7f800000u;
-      odd |= it;
-      x[i] = it ? 0u : x[i];
-    }
-  }
-  return odd;
-}
 
 template <int TYPE, bool Q8, int D, int WQ, int RT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void pages_attend_kernel(AttendArgs a) {
@@ -121,7 +61,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   constexpr bool BF16 = F::kBf16;
   constexpr int TN = F::TN, KT = F::kKeyTiles, NSL = F::kSlabs, NCB = F::kChans, NV = F::kVecs;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ unsigned odd_rows[2][TN / 32];  // of the tile in each stage: rows with values that are not finite
+  __shared__ int any_odd;  // values that are not finite have been taken out of a tile
   const PagesView& c = a.c;
 
   // ---- which query rows, which tiles
@@ -131,26 +71,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wq = wave % WQ, wk = wave / WQ;
-  const int len = pages_len(c, seq), count = chunk_count(a.chunk, seq);
-  const int n_rows = count * a.group, first_row = row_group * F::kRows;
-  if (first_row >= n_rows) return;  // (the rows of a split that are never written are not joined either)
-  const int pos0 = len - count;     // position of the first new token
-  // positions of the first and the last token of the workgroup, and of the wave
-  const int last_row = min(first_row + F::kRows, n_rows) - 1;
-  const int p_lo = pos0 + first_row / a.group, p_hi = pos0 + last_row / a.group;
-  const bool window = a.mask.window > 0;
-  auto end_of = [&](int p) { return a.mask.causal ? min(len, p + 1) : len; };        // rows from here on are hidden,
-  auto begin_of = [&](int p) { return window ? p - a.mask.window + 1 : -0x7fffffff; };  // those before too, but
-  const int sinks = window ? a.mask.n_sink : 0;                                        // the first of all
-  const int hi = end_of(p_hi), lo = begin_of(p_lo);
-  const int sink_tiles = (max(min(sinks, hi), 0) + TN - 1) / TN;
-  const int from_tile = max(max(lo, 0) / TN, sink_tiles), n_tile_all = sink_tiles + max((hi + TN - 1) / TN - from_tile, 0);
-  auto key0_of = [&](int t) { return (t < sink_tiles ? t : from_tile + t - sink_tiles) * TN; };  // first key of tile t
-  const int per = (n_tile_all + a.n_split - 1) / a.n_split;
-  const int t0 = min(split * per, n_tile_all), t1 = min(t0 + per, n_tile_all);
+  const int first_row = row_group * F::kRows, wave_row = first_row + wq * (16 * RT);
+  if (first_row >= chunk_count(a.chunk, seq) * a.group) return;  // (rows of a split that are not written are not joined)
+  const Seen<TN> seen(a, seq, first_row, F::kRows);
+  const int n_rows = seen.n_rows, pos0 = seen.pos0, sinks = seen.sinks;
+  const int per = (seen.n_tile + a.n_split - 1) / a.n_split;
+  const int t0 = min(split * per, seen.n_tile), t1 = min(t0 + per, seen.n_tile);
 
   // ---- the query rows of this lane
-  const int wave_row = first_row + wq * (16 * RT);
   int q_end[RT], q_begin[RT], q_row[RT];
   u32x4 qf[RT][NSL];
 #pragma unroll
@@ -158,19 +86,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const int r = min(wave_row + 16 * b + i, n_rows - 1);
     const int t = r / a.group, head = kv * a.group + (r - t * a.group);
     q_row[b] = r;
-    q_end[b] = end_of(pos0 + t);
-    q_begin[b] = begin_of(pos0 + t);
+    q_end[b] = seen.end_of(pos0 + t);
+    q_begin[b] = seen.begin_of(pos0 + t);
     const long long at = (long long)chunk_first(a.chunk, seq) + t;
     const u32x4* src = (const u32x4*)(a.q.p + seq * a.q.seq + head * a.q.head + at * a.q.row);
     const bool there = at >= 0 && at < a.q.n_row;
 #pragma unroll
     for (int sl = 0; sl < NSL; ++sl) qf[b][sl] = there ? src[4 * sl + g] : u32x4{0, 0, 0, 0};
   }
-  // what all rows of the wave see, and what all rows of the workgroup do: [begin, end) and the first `sinks`
-  const int w_lo = pos0 + min(wave_row, n_rows - 1) / a.group;
-  const int w_hi = pos0 + min(wave_row + 16 * RT - 1, n_rows - 1) / a.group;
-  const int w_end = end_of(w_lo), w_begin = begin_of(w_hi);
-  const int all_end = end_of(p_lo), all_begin = begin_of(p_hi);
+  // what all rows of the wave see: [begin, end) and the first `sinks`
+  const int w_end = seen.end_of(pos0 + min(wave_row, n_rows - 1) / a.group);
+  const int w_begin = seen.begin_of(pos0 + min(wave_row + 16 * RT - 1, n_rows - 1) / a.group);
 
   // ---- tiles: a thread's vectors of a tile lie kThreads vectors apart
   int page[NV];
@@ -180,18 +106,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   constexpr int kRowsApart = kThreads / F::kSrcChunks;
   const int32_t* const table = c.table + (long long)seq * c.width;
   const long long kv_ofs = kv * c.head, kv_scale = kv * c.scale_head;
-  auto visible_here = [&](int pos) { return pos < hi && (pos >= lo || pos < sinks); };
   auto ask_pages = [&](int t) __attribute__((always_inline)) {
-    const int key0 = key0_of(t);
+    const int key0 = seen.key0(t);
 #pragma unroll
     for (int p = 0; p < NV; ++p) {
       const int pos = key0 + ld_row + p * kRowsApart;
       page[p] = -1;
-      if (t < t1 && visible_here(pos)) page[p] = table[pos >> c.page_shift];
+      if (t < t1 && seen.some(pos)) page[p] = table[pos >> c.page_shift];
     }
   };
   auto ask_rows = [&](int t) __attribute__((always_inline)) {
-    const int key0 = key0_of(t);
+    const int key0 = seen.key0(t);
 #pragma unroll
     for (int p = 0; p < NV; ++p) {
       const int slot = (key0 + ld_row + p * kRowsApart) & ((1 << c.page_shift) - 1);
@@ -209,15 +134,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
     }
   };
-  // some rows of the workgroup see a key of tile t that others do not
-  auto is_edge = [&](int t) {
-    const int key0 = key0_of(t), end = min(key0 + TN, hi);
-    return end > all_end || (window && max(key0, lo) < min(all_begin, end) && max(key0, sinks) < min(all_begin, end));
-  };
   auto store_rows = [&](int t, int stage) __attribute__((always_inline)) {
     unsigned char* const k_lds = smem + stage * F::kTileBytes;
     unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
-    const bool edge = is_edge(t);
+    const bool edge = seen.edge(t);
     constexpr int kOut = Q8 ? F::kElem : 1;  // vectors in LDS for one of the cache
 #pragma unroll
     for (int p = 0; p < NV; ++p) {
@@ -234,7 +154,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         bool odd = false;
 #pragma unroll
         for (int w = 0; w < kOut; ++w) odd |= take_odd<BF16>(y[w]);
-        if (odd) atomicOr(&odd_rows[stage][row / 32], 1u << (row % 32));
+        if (odd) any_odd = 1;
       }
 #pragma unroll
       for (int w = 0; w < kOut; ++w) {
@@ -258,45 +178,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // key of register v of key tile t, in a block
   auto key_of = [&](int t, int v) { return BF16 ? 16 * (g & 1) + 8 * (g >> 1) + 4 * t + v : 4 * g + v; };
 
-  // Values that are not finite in rows of an edge tile, for the query rows that see them; w: weights of the block.
-  auto add_odd = [&](int key0, int block, unsigned rows, const float (&w)[RT][4 * KT]) {
-    for (int x = 0; x < 4 * KT; ++x)
-      for (int from = 0; from < 4; ++from) {
-        const int key = BF16 ? 16 * (from & 1) + 8 * (from >> 1) + x : 4 * from + x;
-        if (!(rows >> key & 1)) continue;
-        const int pos = key0 + block * F::kBlock + key, slot = pos & ((1 << c.page_shift) - 1);
-        const int pg = table[pos >> c.page_shift];  // (in the pool: its rows are not all zeros)
-        const unsigned char* src = c.v + (pg * c.page + kv_ofs + slot * F::kSrcRow);
-        float scale = 1.f;
-        if constexpr (Q8) scale = __uint_as_float((unsigned)c.v_scale[pg * c.scale_page + kv_scale + slot] << 23);
-#pragma unroll
-        for (int b = 0; b < RT; ++b) {
-          float weight = 0.f;
-#pragma unroll
-          for (int y = 0; y < 4 * KT; ++y) weight = y == x ? w[b][y] : weight;
-          weight = __shfl(weight, 16 * from + i);
-          const bool sees = pos < q_end[b] && (pos >= q_begin[b] || pos < sinks);
-#pragma unroll
-          for (int ch = 0; ch < NCB; ++ch)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int channel = 16 * ch + 4 * g + v;
-              float val;
-              if constexpr (Q8) val = __builtin_amdgcn_cvt_pk_f32_fp8(src[channel], false)[0] * scale;
-              else if constexpr (BF16) val = __uint_as_float((unsigned)((const uint16_t*)src)[channel] << 16);
-              else val = ((const float*)src)[channel];
-              if (sees && !(fabsf(val) < INFINITY)) o[b][ch][v] += weight * val;
-            }
-        }
-      }
-  };
-
   auto work = [&](int t, int stage) __attribute__((always_inline)) {
     const unsigned char* const k_lds = smem + stage * F::kTileBytes;
     const unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
-    const int key0 = key0_of(t);
-    const bool masked = key0 + TN > w_end || (window && key0 < w_begin && key0 + TN > sinks);
-    const bool edge = is_edge(t);
+    const int key0 = seen.key0(t);
+    const bool masked = key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > sinks);
 #pragma unroll
     for (int nb = 0; nb < F::kBlocks; ++nb) {
       const int block = wk * F::kBlocks + nb;
@@ -401,28 +287,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
           }
         }
       }
-      if (edge) {
-        const unsigned rows = odd_rows[stage][block * F::kBlock / 32] >> (block * F::kBlock % 32);
-        const unsigned mine = __builtin_amdgcn_readfirstlane(BF16 ? rows : rows & 0xffffu);
-        if (mine) {
-#pragma unroll
-          for (int b = 0; b < RT; ++b)
-#pragma unroll
-            for (int y = 0; y < 4 * KT; ++y)
-              if constexpr (BF16) w[b][y] = (float)(__bf16)w[b][y];
-          add_odd(key0, block, mine, w);
-        }
-      }
     }
   };
 
   // ---- the tiles
-  auto clear_odd = [&](int stage) {
-    if (tid < TN / 32) odd_rows[stage][tid] = 0;
-  };
+  if (tid == 0) any_odd = 0;
   if (t0 < t1) {
-    clear_odd(0);
-    if (F::kStages > 1) clear_odd(1);
     ask_pages(t0);
     ask_rows(t0);
     ask_pages(t0 + 1);
@@ -437,21 +307,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
       if (wave_row < n_rows) work(t, stage);  // (the others only carry their share of the tiles)
       if constexpr (F::kStages > 1) {
-        // (the other stage was left before the last barrier; what is remembered of this tile's rows is cleared after
-        // the next one, two tiles before it is written again)
-        if (t + 1 < t1) store_rows(t + 1, stage ^ 1);
-        __syncthreads();
-        if (is_edge(t)) clear_odd(stage);
-        if (t + 2 < t1 && is_edge(t)) __syncthreads();
+        if (t + 1 < t1) store_rows(t + 1, stage ^ 1);  // (left by all waves before the last barrier)
       } else {
         __syncthreads();
-        if (is_edge(t)) {
-          clear_odd(0);
-          __syncthreads();
-        }
         if (t + 1 < t1) store_rows(t + 1, 0);
-        __syncthreads();
       }
+      __syncthreads();
+    }
+    if (any_odd && wave_row < n_rows) {
+      float less[RT];
+#pragma unroll
+      for (int b = 0; b < RT; ++b) less[b] = -(m_run[b] * a.scale_log2e);
+      float* const sums = (float*)smem + wave * (16 * RT * D);
+      sums_to_lds<D, RT>(o, sums);
+      constexpr int kMine = F::kBlocks * F::kBlock;
+      add_odd<TYPE, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t1, wk * kMine, (wk + 1) * kMine, less, sums);
+      sums_from_lds<D, RT>(o, sums);
     }
   }
 
@@ -501,7 +372,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (a.n_split > 1) {
       const long long row = ((long long)unit * a.chunk.max_new * a.group + r) * a.n_split + split;
       if (g == 0) {
-        a.stat[2 * row] = m_run[b];
+        a.stat[2 * row] = m_run[b] * a.scale_log2e;
         a.stat[2 * row + 1] = l_run[b];
       }
 #pragma unroll
@@ -540,13 +411,13 @@ __global__ __launch_bounds__(kThreads) void pages_join_kernel(AttendArgs a, int 
   if (at < 0 || at >= a.out.n_row) return;
   const float* stat = a.stat + 2LL * row * a.n_split;
   const float* part = a.part + (long long)row * a.n_split * D + kPer * lane;
-  float top = a.no_max;
+  float top = -INFINITY;
   for (int x = 0; x < a.n_split; ++x) top = fmaxf(top, stat[2 * x]);
   float sum = 0.f, o[kPer] = {};
   for (int x = 0; x < a.n_split; ++x) {
     const float l = stat[2 * x + 1];
     if (l == 0.f) continue;  // no keys there, or none of any weight
-    const float f = __builtin_amdgcn_exp2f((stat[2 * x] - top) * a.scale_log2e);
+    const float f = __builtin_amdgcn_exp2f(stat[2 * x] - top);
     sum += f * l;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] += f * part[(long long)x * D + e];
@@ -573,8 +444,7 @@ hipError_t launch_form(const AttendArgs& a, hipStream_t stream) {
 template <int TYPE, bool Q8, int D>
 hipError_t launch_plan(const PagesPlan& plan, const AttendArgs& a, hipStream_t stream) {
   if constexpr (TYPE == kTypeBf16) {
-    if (plan.row_waves == 4)
-      return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 4, 2>(a, stream) : launch_form<TYPE, Q8, D, 4, 1>(a, stream);
+    if (plan.row_waves == 4) return launch_pages_chunk(D, Q8, plan.row_tiles, a, stream);
     return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 1, 2>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);
   } else {
     return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4, 1>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);

@@ -1,0 +1,553 @@
+// Attention over pages for many query rows (bf16 arithmetic): the products and the schedule of the pipelined dense
+// kernel (attend_pipe.hip: three blocks of 32 keys under way in a wave, an MFMA, a request to the LDS and a step of the
+// softmax in turn), with rows fetched from pages, masks, and shared KV heads.
+//
+// Four waves of 16 RT query rows each share tiles of 64 keys, in two stages.  A wave brings in 16 rows of a tile: they
+// lie in one page whatever its size (16 rows or more), so that the page's number and the rows' address are scalars.
+// bf16 rows go straight into LDS; e4m3 rows pass through registers, where they become bf16 once for the four waves
+// (exactly), requested a tile ahead.  A wave whose 16 rows some lanes must not read (behind the last row, outside
+// window and sinks) fetches zeros for those; pages that do not exist are zeros too.
+//
+// Running maximum: formed per lane (an eighth of a block's keys), it is joined over the four lanes of a row only where it
+// exceeds the row's offset by kRescaleThreshold log2 units in some row of the wave, which after the first blocks is rare;
+// the accumulators are rescaled behind the product that is then still to come with the old offset.
+#include <type_traits>
+
+#include "pages_attend.h"
+
+namespace scalekv {
+namespace {
+
+constexpr int TN = 64;   // keys of a tile
+constexpr int kWaves = 4;
+
+// sixteen cached rows of zeros, in the place of what is not there
+__device__ __attribute__((aligned(256))) const unsigned char g_zero_rows[16 * 256] = {};
+
+template <int D, bool Q8, int RT>
+struct Chunk {
+  static constexpr int kRowBytes = 2 * D;              // in LDS
+  static constexpr int kTileBytes = TN * kRowBytes;
+  static constexpr int kSlabs = D / 32;
+  static constexpr int kBlocks = D / 16;
+  static constexpr int kChunks = D / 8;
+  static constexpr int kRowsPerOp = 64 / kChunks;      // bf16: rows that one transfer of a wave covers
+  static constexpr int kOps = 16 / kRowsPerOp;
+  static constexpr int kVecs = 16 * D / 16 / 64;       // e4m3: 16-byte vectors of a lane for 16 rows (2, 1)
+  static constexpr int kRows = 16 * RT * kWaves;
+  static constexpr int kWavesPerSimd = D == 128 ? 2 : 3;
+  static constexpr int kLds = 4 * kTileBytes;          // two stages of K, two of V
+  static_assert(kWaves * 16 * RT * D * 4 <= kLds, "the sums of all waves fit (add_odd)");
+};
+
+// 16 bytes a lane from base + voff straight into LDS, at lds_addr + 16 lane (attend_pipe.hip has the reasons for assembly);
+// the first with a base of the wave, the second with an address of the lane
+template <int IMM>
+__device__ __forceinline__ void dma16(const unsigned char* base_uniform, unsigned voff, unsigned lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+               :: "s"(lds_addr_uniform), "v"(voff), "s"(base_uniform), "n"(IMM) : "m0", "memory");
+}
+__device__ __forceinline__ void dma16_lane(const unsigned char* address, unsigned lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_addr_uniform), "v"(address) : "m0", "memory");
+}
+
+template <int D, bool Q8, int RT>
+__global__ __launch_bounds__(64 * kWaves)
+__attribute__((amdgpu_waves_per_eu(Chunk<D, Q8, RT>::kWavesPerSimd, Chunk<D, Q8, RT>::kWavesPerSimd)))
+void pages_chunk_kernel(AttendArgs a) {
+  using G = Chunk<D, Q8, RT>;
+  constexpr int kRowBytes = G::kRowBytes, kTileBytes = G::kTileBytes, NSL = G::kSlabs, NCB = G::kBlocks;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ long long row_at[G::kRows];                  // byte offset of each output row, -1: none
+  __shared__ int row_end[G::kRows], row_begin[G::kRows];  // what each row sees
+  __shared__ int any_odd;                                 // values that are not finite have been taken out of a tile
+  const PagesView& c = a.c;
+
+  const int wg = xcd_order(SCALEKV_WG_X, a.n_wg);  // row groups of a unit share an L2
+  const int split = wg % a.n_split, unit = wg / a.n_split / a.n_row_group;
+  // under a causal mask later rows see more: they come first, so that the short ones fill up the end
+  const int nth = wg / a.n_split % a.n_row_group, row_group = a.mask.causal ? a.n_row_group - 1 - nth : nth;
+  const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first_row = row_group * G::kRows, wave_row = first_row + wave * (16 * RT);
+  if (first_row >= chunk_count(a.chunk, seq) * a.group) return;
+  const Seen<TN> seen(a, seq, first_row, G::kRows);
+  const int per = (seen.n_tile + a.n_split - 1) / a.n_split;
+  const int t0 = min(split * per, seen.n_tile), n_tile = min(t0 + per, seen.n_tile) - t0;
+  // all rows of the wave see [w_begin, w_end) and the sinks below w_end
+  const int w_end = seen.end_of(seen.pos0 + min(wave_row, seen.n_rows - 1) / a.group);
+  const int w_begin = seen.begin_of(seen.pos0 + min(wave_row + 16 * RT - 1, seen.n_rows - 1) / a.group);
+
+  // ---- query rows: B operand of the first product, resident
+  bf16x8 qf[RT][NSL];
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+    const int r = min(wave_row + 16 * b + i, seen.n_rows - 1), t = r / a.group, head = kv * a.group + (r - t * a.group);
+    const long long at = (long long)chunk_first(a.chunk, seq) + t;
+    const u32x4* src = (const u32x4*)(a.q.p + seq * a.q.seq + head * a.q.head + at * a.q.row);
+    const bool there = at >= 0 && at < a.q.n_row;
+#pragma unroll
+    for (int sl = 0; sl < NSL; ++sl) qf[b][sl] = __builtin_bit_cast(bf16x8, there ? src[4 * sl + g] : u32x4{0, 0, 0, 0});
+    if (g == 0) {
+      const int slot = 16 * (RT * wave + b) + i;
+      const bool store = wave_row + 16 * b + i < seen.n_rows && at >= 0 && at < a.out.n_row;
+      row_at[slot] = store ? seq * a.out.seq + head * a.out.head + at * a.out.row : -1;
+      row_end[slot] = seen.end_of(seen.pos0 + t);
+      row_begin[slot] = seen.begin_of(seen.pos0 + t);
+    }
+  }
+  if (tid == 0) any_odd = 0;
+
+  // ---- tiles
+  auto lds_addr = [](const unsigned char* p) -> unsigned {
+    return (unsigned)(size_t)(const __attribute__((address_space(3))) unsigned char*)p;
+  };
+  unsigned char* const k_lds = smem;
+  unsigned char* const v_lds = smem + 2 * kTileBytes;
+  const int32_t* const table = c.table + (long long)seq * c.width;
+  const long long kv_ofs = kv * c.head;
+  auto key0_of = [&](int t) { return seen.key0(t0 + t); };
+  // the page of this wave's rows of tile t; any number outside the pool stands for rows of zeros
+  auto ask_page = [&](int t) -> int {
+    const int pos = key0_of(t) + 16 * wave;
+    return t < n_tile && seen.any(pos, 16) ? table[pos >> c.page_shift] : -1;
+  };
+  int page_next = -1;  // of the tile whose K rows are requested next (as it was loaded; made a scalar when it is used)
+  int page_k = -1;     // of the tile before: its V rows are requested with them
+  // this wave's rows of a tensor
+  auto rows_at = [&](const unsigned char* pool, int page, int t) -> const unsigned char* {
+    const int slot = (key0_of(t) + 16 * wave) & ((1 << c.page_shift) - 1);
+    return scalar((unsigned)page < (unsigned)c.n_page ? pool + page * c.page + kv_ofs + slot * (Q8 ? D : kRowBytes)
+                                                      : g_zero_rows);
+  };
+  // bf16: instruction p fills LDS rows 16 wave + kRowsPerOp p ..; the lane that lands in chunk slot s of row r fetches
+  // chunk s ^ flip(r)
+  const int ld_row = lane / G::kChunks;
+  const unsigned ld_k = ld_row * kRowBytes, ld_kchunk = 16 * ((lane % G::kChunks) ^ k_flip_bf16<D>(16 * wave + ld_row));
+  const unsigned ld_v = ld_row * kRowBytes + 16 * ((lane % G::kChunks) ^ v_flip_bf16<D>(16 * wave + ld_row));
+  constexpr auto k_step = [](int p) -> unsigned { return 16 * k_flip_bf16<D>(G::kRowsPerOp * p); };
+  const unsigned k_wave = __builtin_amdgcn_readfirstlane(lds_addr(k_lds + 16 * wave * kRowBytes));
+  const unsigned v_wave = __builtin_amdgcn_readfirstlane(lds_addr(v_lds + 16 * wave * kRowBytes));
+  auto transfer = [&](const unsigned char* rows, int t, unsigned dst, auto ofs) __attribute__((always_inline)) {
+    if (seen.every(key0_of(t) + 16 * wave, 16)) {
+      // (the immediate offset moves the destination along with the source)
+      dma16<0>(rows, ofs(0), dst);
+      dma16<1024>(rows, ofs(1), dst);
+      if constexpr (G::kOps == 4) {
+        dma16<2048>(rows, ofs(2), dst);
+        dma16<3072>(rows, ofs(3), dst);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < G::kOps; ++p) {
+        const bool there = seen.some(key0_of(t) + 16 * wave + G::kRowsPerOp * p + ld_row);
+        dma16_lane((there ? rows : (const unsigned char*)g_zero_rows) + ofs(p) + 1024 * p, dst + 1024 * p);
+      }
+    }
+  };
+  // e4m3: a lane has kVecs vectors of 16 codes; vector p lies in row 16 wave + (16 / kVecs) p + lane / (D / 16)
+  constexpr int kSrcChunks = D / 16, kVecRows = 16 / G::kVecs;
+  const int q8_row = lane / kSrcChunks, q8_chunk = lane % kSrcChunks;
+  u32x4 k_raw[G::kVecs], v_raw[G::kVecs];
+  uint8_t k_sc[G::kVecs], v_sc[G::kVecs];
+  auto fetch = [&](const unsigned char* pool, const uint8_t* scales, int page, int t, u32x4 (&raw)[G::kVecs],
+                   uint8_t (&sc)[G::kVecs]) __attribute__((always_inline)) {
+    const int pos = key0_of(t) + 16 * wave, slot = pos & ((1 << c.page_shift) - 1);
+    const bool in_pool = (unsigned)page < (unsigned)c.n_page;
+    const unsigned char* rows = rows_at(pool, page, t);
+    const uint8_t* scale = in_pool ? scales + page * c.scale_page + kv * c.scale_head + slot : (const uint8_t*)g_zero_rows;
+#pragma unroll
+    for (int p = 0; p < G::kVecs; ++p) {
+      raw[p] = *(const u32x4*)(rows + 1024 * p + 16 * lane);
+      sc[p] = scale[kVecRows * p + q8_row];
+      if (!seen.every(pos, 16) && !seen.some(pos + kVecRows * p + q8_row)) raw[p] = u32x4{0, 0, 0, 0};
+    }
+  };
+  auto put = [&](unsigned char* stage, const u32x4 (&raw)[G::kVecs], const uint8_t (&sc)[G::kVecs], bool values, bool edge)
+                 __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < G::kVecs; ++p) {
+      const int row = 16 * wave + kVecRows * p + q8_row;
+      u32x4 x[2];
+      widen(raw[p], __uint_as_float((unsigned)sc[p] << 23), x);
+      if (values && edge && (take_odd<true>(x[0]) | take_odd<true>(x[1]))) any_odd = 1;
+      const int flip = values ? v_flip_bf16<D>(row) : k_flip_bf16<D>(row);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) *(u32x4*)(stage + row * kRowBytes + 16 * ((2 * q8_chunk + w) ^ flip)) = x[w];
+      __builtin_amdgcn_sched_barrier(0);  // (a vector at a time: registers are scarce here)
+    }
+  };
+  auto issue_k = [&](int t, int page) __attribute__((always_inline)) {
+    if constexpr (Q8) fetch(c.k, c.k_scale, page, t, k_raw, k_sc);
+    else
+      transfer(rows_at(c.k, page, t), t, k_wave + (t & 1) * kTileBytes,
+               [&](int p) { return ld_k + (ld_kchunk ^ k_step(p)); });
+  };
+  auto issue_v = [&](int t, int page) __attribute__((always_inline)) {
+    if constexpr (Q8) fetch(c.v, c.v_scale, page, t, v_raw, v_sc);
+    else transfer(rows_at(c.v, page, t), t, v_wave + (t & 1) * kTileBytes, [&](int) { return ld_v; });
+  };
+  auto put_k = [&](int t) { put(k_lds + (t & 1) * kTileBytes, k_raw, k_sc, false, false); };
+  auto put_v = [&](int t) { put(v_lds + (t & 1) * kTileBytes, v_raw, v_sc, true, seen.edge(t0 + t)); };
+  // bf16: values of an edge tile that are not finite, in the rows that this wave has brought in
+  auto sift = [&](int t) {
+    unsigned char* const mine = v_lds + (t & 1) * kTileBytes + 16 * wave * kRowBytes + 16 * lane;
+    for (int p = 0; p < G::kOps; ++p) {
+      u32x4 x = *(const u32x4*)(mine + 1024 * p);
+      if (take_odd<true>(x)) {
+        *(u32x4*)(mine + 1024 * p) = x;
+        any_odd = 1;
+      }
+    }
+  };
+
+  // ---- operand addresses in the first block of 32 keys; key tile t is 4 rows further on
+  unsigned k_adr[NSL], v_adr[NCB];
+  {
+    const int row = 16 * (i >> 2 & 1) + 8 * (i >> 3) + (i & 3);
+#pragma unroll
+    for (int sl = 0; sl < NSL; ++sl) k_adr[sl] = lds_addr(k_lds) + row * kRowBytes + 16 * ((4 * sl + g) ^ k_flip_bf16<D>(row));
+  }
+  {
+    const int row = 16 * (g & 1) + 8 * (g >> 1) + (i >> 2);
+#pragma unroll
+    for (int x = 0; x < NCB; ++x) v_adr[x] = lds_addr(v_lds) + row * kRowBytes + 16 * (2 * x ^ v_flip_bf16<D>(row)) + 8 * (i & 3);
+  }
+#pragma unroll
+  for (int sl = 0; sl < NSL; ++sl) asm volatile("" : "+v"(k_adr[sl]));
+#pragma unroll
+  for (int x = 0; x < NCB; ++x) asm volatile("" : "+v"(v_adr[x]));
+
+  f32x4 o[RT][NCB];
+  float neg[RT], l_run[RT], alpha[RT];  // less the rows' offsets (log2 units), this lane's share of the sums
+  bool moved = false;                   // offsets have moved: the accumulators are to be scaled by alpha
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+#pragma unroll
+    for (int x = 0; x < NCB; ++x) o[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    neg[b] = -(a.no_max * a.scale_log2e);
+    l_run[b] = 0.f;
+    alpha[b] = 1.f;
+  }
+
+  typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  constexpr int kHalf = 32 * kRowBytes;
+  constexpr int kSlots = 2 * NSL * RT;      // MFMAs of one product over a block
+  constexpr int kSteps = 8 * RT / kSlots;   // softmax steps behind each
+  constexpr int kKReads = 2 * NSL, kVReads = 2 * NCB;
+  constexpr int kBarrierSlot = kSlots / 2 - 1;
+  bf16x8 kf[2][NSL];
+  s16x4 vf[NCB][2];
+  f32x4 sa[RT][2], sb[RT][2];
+  u32x4 pa[RT], pb[RT];
+
+  auto read_k = [&](int ofs, int e) { kf[e & 1][e >> 1] = *(lds_bf16x8*)(k_adr[e >> 1] + ofs + 4 * (e & 1) * kRowBytes); };
+  auto read_v = [&](int ofs, int e) {
+    vf[e >> 1][e & 1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_adr[e >> 1] + ofs + 4 * (e & 1) * kRowBytes));
+  };
+  auto score_mfma = [&](f32x4 (&s)[RT][2], int m) {
+    const int sl = m / (2 * RT), t = m / RT % 2, b = m % RT;
+    const f32x4 sum = sl ? s[b][t] : f32x4{0.f, 0.f, 0.f, 0.f};
+    s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][sl], qf[b][sl], sum, 0, 0, 0);
+  };
+  auto value_mfma = [&](const u32x4 (&p)[RT], int m) {
+    const int x = m / RT, b = m % RT;
+    const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vf[x][0], vf[x][1], 0, 1, 2, 3, 4, 5, 6, 7));
+    o[b][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, p[b]), o[b][x], 0, 0, 0);
+  };
+  // Step k of 16 RT of a block's softmax: four for each pair of weights.  (The empty statements keep each step in its slot.)
+  auto softmax_step = [&](f32x4 (&s)[RT][2], u32x4 (&p)[RT], int k) {
+    const int b = k >> 4, x = 2 * (k >> 2 & 3), t = x >> 2, v = x & 3;
+    float w0 = s[b][t][v], w1 = s[b][t][v + 1];
+    if ((k & 3) == 0) {
+      w0 = fmaf(w0, a.scale_log2e, neg[b]);
+      w1 = fmaf(w1, a.scale_log2e, neg[b]);
+      asm volatile("" : "+v"(w0), "+v"(w1));
+    } else if ((k & 3) == 1) {
+      w0 = __builtin_amdgcn_exp2f(w0);
+      asm volatile("" : "+v"(w0));
+    } else if ((k & 3) == 2) {
+      w1 = __builtin_amdgcn_exp2f(w1);
+      asm volatile("" : "+v"(w1));
+    } else {
+      // (weights are rounded to bf16 for the matrix cores; the sum adds the rounded ones)
+      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f}, pr = {(__bf16)w0, (__bf16)w1};
+      uint32_t word = __builtin_bit_cast(uint32_t, pr);
+      l_run[b] = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run[b], false);
+      asm volatile("" : "+v"(word), "+v"(l_run[b]));
+      p[b][x / 2] = word;
+    }
+    s[b][t][v] = w0;
+    s[b][t][v + 1] = w1;
+  };
+  // Before the softmax of a block (half h of tile t): hide what its rows do not see, and move the offsets if need be.
+  auto prepare = [&](f32x4 (&s)[RT][2], int t, int h) __attribute__((always_inline)) {
+    const int key0 = key0_of(t);
+    if (key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > seen.sinks)) {
+      const int mine = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+      const int pos0 = key0 + 32 * h + 16 * (mine >> 4 & 1) + 8 * (mine >> 5);
+#pragma unroll
+      for (int b = 0; b < RT; ++b) {
+        const int end = row_end[16 * (RT * wave + b) + (mine & 15)], begin = row_begin[16 * (RT * wave + b) + (mine & 15)];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int pos = pos0 + x;
+          if (pos >= end || (pos < begin && pos >= seen.sinks)) s[b][x / 4][x % 4] = -INFINITY;
+        }
+      }
+    }
+    float mx[RT];
+    bool grow = false;
+#pragma unroll
+    for (int b = 0; b < RT; ++b) {
+      mx[b] = s[b][0][0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) mx[b] = fmaxf(mx[b], s[b][x / 4][x % 4]);
+      grow |= fmaf(mx[b], a.scale_log2e, neg[b]) > kRescaleThreshold;
+    }
+    moved = __builtin_amdgcn_ballot_w64(grow) != 0;
+    if (moved) {
+#pragma unroll
+      for (int b = 0; b < RT; ++b) {
+        const float now = fminf(neg[b], -(xor32_max(xor16_max(mx[b])) * a.scale_log2e));
+        alpha[b] = __builtin_amdgcn_exp2f(now - neg[b]);
+        neg[b] = now;
+        l_run[b] *= alpha[b];
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto rescale = [&]() __attribute__((always_inline)) {
+    if (moved) {
+#pragma unroll
+      for (int b = 0; b < RT; ++b)
+#pragma unroll
+        for (int x = 0; x < NCB; ++x) o[b][x] *= alpha[b];
+    }
+  };
+  auto slots = [&](auto mfma, auto beside, f32x4 (&s)[RT][2], u32x4 (&p)[RT], int first_step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < kSlots; ++m) {
+      mfma(m);
+      beside(m);
+#pragma unroll
+      for (int r = 0; r < kSteps; ++r) softmax_step(s, p, first_step + m * kSteps + r);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Publishes tile t + 1 of K and tile t of V, and requests the tiles behind them in the place of those that all waves
+  // have left.
+  auto turn = [&](int t) __attribute__((always_inline)) {
+    if constexpr (Q8) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what this wave has put is there
+      __syncthreads();
+      if (t + 1 < n_tile) put_v(t + 1);
+      if (t + 2 < n_tile) put_k(t + 2);
+      if (t + 2 < n_tile) issue_v(t + 2, page_k);
+      const int page = __builtin_amdgcn_readfirstlane(page_next);
+      if (t + 3 < n_tile) issue_k(t + 3, page);
+      page_k = page;
+      page_next = ask_page(t + 4);
+    } else {
+      __builtin_amdgcn_s_waitcnt(0);
+      if (seen.edge(t0 + t)) {
+        sift(t);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+      }
+      __syncthreads();
+      if (t + 1 < n_tile) issue_v(t + 1, page_k);
+      const int page = __builtin_amdgcn_readfirstlane(page_next);
+      if (t + 2 < n_tile) issue_k(t + 2, page);
+      page_k = page;
+      page_next = ask_page(t + 3);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto nothing = [](int) {};
+  auto first_half = [&](int t, int st) __attribute__((always_inline)) {
+    prepare(sa, t, 0);
+    slots([&](int m) { score_mfma(sb, m); },
+          [&](int m) {
+#pragma unroll
+            for (int e = m * kVReads / kSlots; e < (m + 1) * kVReads / kSlots; ++e) read_v((st ^ 1) * kTileBytes + kHalf, e);
+          },
+          sa, pa, 0);
+    slots([&](int m) { value_mfma(pb, m); },
+          [&](int m) {
+            if (m == kBarrierSlot) turn(t);
+            if (m > kBarrierSlot) {
+              constexpr int kLeft = kSlots - kBarrierSlot - 1;
+              const int x = m - kBarrierSlot - 1;
+#pragma unroll
+              for (int e = x * kKReads / kLeft; e < (x + 1) * kKReads / kLeft; ++e) read_k((st ^ 1) * kTileBytes, e);
+            }
+          },
+          sa, pa, 8 * RT);
+    rescale();
+  };
+  auto second_half = [&](int t, int st) __attribute__((always_inline)) {
+    prepare(sb, t, 1);
+    slots([&](int m) { score_mfma(sa, m); },
+          [&](int m) {
+#pragma unroll
+            for (int e = m * kVReads / kSlots; e < (m + 1) * kVReads / kSlots; ++e) read_v(st * kTileBytes, e);
+          },
+          sb, pb, 0);
+    slots([&](int m) { value_mfma(pa, m); },
+          [&](int m) { if (m < kKReads) read_k((st ^ 1) * kTileBytes + kHalf, m); }, sb, pb, 8 * RT);
+    rescale();
+  };
+
+  if (n_tile > 0) {
+    {
+      const int p0 = __builtin_amdgcn_readfirstlane(ask_page(0)), p1 = __builtin_amdgcn_readfirstlane(ask_page(1));
+      __syncthreads();  // (any_odd and the rows' tables are written)
+      if constexpr (Q8) {
+        const int p2 = __builtin_amdgcn_readfirstlane(ask_page(2));
+        issue_k(0, p0);
+        issue_v(0, p0);
+        put_k(0);
+        put_v(0);
+        if (n_tile > 1) {
+          issue_k(1, p1);
+          put_k(1);
+          issue_v(1, p1);
+        }
+        if (n_tile > 2) issue_k(2, p2);
+        page_k = p2;
+        page_next = ask_page(3);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+      } else {
+        issue_k(0, p0);
+        issue_v(0, p0);
+        if (n_tile > 1) issue_k(1, p1);
+        page_k = p1;
+        page_next = ask_page(2);
+        __builtin_amdgcn_s_waitcnt(0);
+      }
+    }
+    __syncthreads();
+    if (wave_row < seen.n_rows) {
+#pragma unroll
+      for (int e = 0; e < kKReads; ++e) read_k(0, e);
+#pragma unroll
+      for (int m = 0; m < kSlots; ++m) score_mfma(sa, m);
+#pragma unroll
+      for (int e = 0; e < kKReads; ++e) read_k(kHalf, e);
+#pragma unroll
+      for (int m = 0; m < kSlots; ++m) score_mfma(sb, m);
+      prepare(sa, 0, 0);
+      slots(nothing, nothing, sa, pa, 0);
+      turn(0);
+      slots(nothing, [&](int m) { if (m < kKReads) read_k(kTileBytes, m); }, sa, pa, 8 * RT);
+      // (K of the second tile: its first half; the second half is read beside the first product that takes it)
+      int t = 0;
+      for (; t + 2 < n_tile; t += 2) {
+        second_half(t, 0);
+        first_half(t + 1, 1);
+        second_half(t + 1, 1);
+        first_half(t + 2, 0);
+      }
+      if (t + 1 < n_tile) {
+        second_half(t, 0);
+        first_half(t + 1, 1);
+        ++t;
+      }
+      const int ofs = (t & 1) * kTileBytes;
+      prepare(sb, t, 1);
+      slots(nothing,
+            [&](int m) {
+#pragma unroll
+              for (int e = m * kVReads / kSlots; e < (m + 1) * kVReads / kSlots; ++e) read_v(ofs, e);
+            },
+            sb, pb, 0);
+      slots([&](int m) { value_mfma(pa, m); }, nothing, sb, pb, 8 * RT);
+      rescale();
+#pragma unroll
+      for (int e = 0; e < kVReads; ++e) read_v(ofs + kHalf, e);
+#pragma unroll
+      for (int m = 0; m < kSlots; ++m) value_mfma(pb, m);
+    } else {
+      for (int t = 0; t < n_tile; ++t) turn(t);  // (a wave without rows only carries its share of the tiles)
+    }
+  }
+  __syncthreads();  // all waves have left the tiles
+  if (wave_row >= seen.n_rows) return;
+  // (each wave has a part of the LDS to itself from here on, for add_odd() and then for its output)
+  unsigned char* const mine = smem + wave * (16 * RT * D * 4);
+  if (n_tile > 0 && any_odd) {
+    float* const sums = (float*)mine;
+    sums_to_lds<D, RT>(o, sums);
+    add_odd<kTypeBf16, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t0 + n_tile, 0, TN, neg, sums);
+    sums_from_lds<D, RT>(o, sums);
+  }
+
+  // ---- write
+#pragma unroll
+  for (int b = 0; b < RT; ++b) l_run[b] = xor32_sum(xor16_sum(l_run[b]));
+  if (a.n_split > 1) {
+#pragma unroll
+    for (int b = 0; b < RT; ++b) {
+      const int r = wave_row + 16 * b + i;
+      if (r >= seen.n_rows) continue;
+      const long long row = ((long long)unit * a.chunk.max_new * a.group + r) * a.n_split + split;
+      if (g == 0) {
+        a.stat[2 * row] = -neg[b];
+        a.stat[2 * row + 1] = l_run[b];
+      }
+#pragma unroll
+      for (int x = 0; x < NCB; ++x) *(f32x4*)(a.part + row * D + 16 * x + 4 * g) = o[b][x];
+    }
+    return;
+  }
+  // whole rows through LDS, padded by 16 bytes against bank conflicts
+  constexpr int kOutStride = kRowBytes + 16;
+  static_assert(kOutStride <= D * 4, "the output of a wave fits in its part");
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+    // a row that sees nothing, or keys of weight zero only, is zero
+    const bool empty = l_run[b] == 0.f;
+    const float inv = 1.f / l_run[b];
+#pragma unroll
+    for (int x = 0; x < NCB; ++x) {
+      const f32x4 y = empty ? f32x4{0.f, 0.f, 0.f, 0.f} : o[b][x] * inv;
+      const bf16x2 lo = {(__bf16)y[0], (__bf16)y[1]}, hi = {(__bf16)y[2], (__bf16)y[3]};
+      *(uint2*)(mine + (16 * b + i) * kOutStride + 32 * x + 8 * g) =
+          make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+  for (int p = 0; p < 16 * RT / G::kRowsPerOp; ++p) {
+    const int r = G::kRowsPerOp * p + lane / G::kChunks;
+    const u32x4 val = *(const u32x4*)(mine + r * kOutStride + 16 * (lane % G::kChunks));
+    const long long at = row_at[16 * RT * wave + r];
+    if (at >= 0) *(u32x4*)(a.out.p + at + 16 * (lane % G::kChunks)) = val;
+  }
+}
+
+template <int D, bool Q8, int RT>
+hipError_t launch_form(const AttendArgs& a, hipStream_t stream) {
+  using G = Chunk<D, Q8, RT>;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_dynamic_lds((const void*)pages_chunk_kernel<D, Q8, RT>, G::kLds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((pages_chunk_kernel<D, Q8, RT>), dim3(a.n_wg), dim3(64 * kWaves), G::kLds, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, hipStream_t stream) {
+  auto tiles = [&](auto dim, auto quantised) {
+    return row_tiles == 2 ? launch_form<dim(), quantised(), 2>(a, stream) : launch_form<dim(), quantised(), 1>(a, stream);
+  };
+  auto cache = [&](auto dim) { return q8 ? tiles(dim, std::true_type{}) : tiles(dim, std::false_type{}); };
+  return d == 64 ? cache(std::integral_constant<int, 64>{}) : cache(std::integral_constant<int, 128>{});
+}
+
+}  // namespace scalekv
