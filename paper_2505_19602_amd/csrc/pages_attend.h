@@ -23,6 +23,21 @@ struct AttendArgs {
 // bf16, many query rows (pages_chunk.hip): 64 row_tiles rows to a workgroup
 hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, hipStream_t stream);
 
+// Which unit a workgroup works on, and which part of it: units are dealt out to the XCDs in turn (consecutive workgroup ids go
+// round-robin over them), so that the workgroups of a unit share an L2 and the units of a long sequence do not.
+__device__ __forceinline__ void unit_of(int wg, int n_wg, int per_unit, int& unit, int& part) {
+  const int dealt = n_wg / per_unit / kXcds * kXcds;  // units of whole rounds; the rest one behind the other
+  if (wg < dealt * per_unit) {
+    const int nth = wg / kXcds;
+    unit = nth / per_unit * kXcds + wg % kXcds;
+    part = nth % per_unit;
+  } else {
+    const int rest = wg - dealt * per_unit;
+    unit = dealt + rest / per_unit;
+    part = rest % per_unit;
+  }
+}
+
 // The query rows [first_row, first_row + rows) of a unit (rows: token t, head h of the group, number t * group + h), what
 // they see, and the tiles of TN keys that hold it: those of the sinks, then those from the window's first row on.
 template <int TN>

@@ -65,8 +65,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const PagesView& c = a.c;
 
   // ---- which query rows, which tiles
-  const int wg = xcd_order(SCALEKV_WG_X, a.n_wg);
-  const int split = wg % a.n_split, row_group = wg / a.n_split % a.n_row_group, unit = wg / a.n_split / a.n_row_group;
+  int unit, part_of;
+  unit_of(SCALEKV_WG_X, a.n_wg, a.n_split * a.n_row_group, unit, part_of);
+  const int split = part_of % a.n_split, row_group = part_of / a.n_split;
   const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -4,8 +4,8 @@
 //
 // Four waves of 16 RT query rows each share tiles of 64 keys, in two stages.  A wave brings in 16 rows of a tile: they
 // lie in one page whatever its size (16 rows or more), so that the page's number and the rows' address are scalars.
-// bf16 rows go straight into LDS; e4m3 rows pass through registers, where they become bf16 once for the four waves
-// (exactly), requested a tile ahead.  A wave whose 16 rows some lanes must not read (behind the last row, outside
+// Rows go straight into LDS.  e4m3 rows wait there as codes, a tile ahead, until the wave that has brought them widens
+// them into the tile, once for the four waves (exactly).  A wave whose 16 rows some lanes must not read (behind the last row, outside
 // window and sinks) fetches zeros for those; pages that do not exist are zeros too.
 //
 // Running maximum: formed per lane (an eighth of a block's keys), it is joined over the four lanes of a row only where it
@@ -36,7 +36,7 @@ struct Chunk {
   static constexpr int kVecs = 16 * D / 16 / 64;       // e4m3: 16-byte vectors of a lane for 16 rows (2, 1)
   static constexpr int kRows = 16 * RT * kWaves;
   static constexpr int kWavesPerSimd = D == 128 ? 2 : 3;
-  static constexpr int kLds = 4 * kTileBytes;          // two stages of K, two of V
+  static constexpr int kLds = 4 * kTileBytes + (Q8 ? 2 * kWaves * 16 * D : 0);  // two stages of K, two of V; codes
   static_assert(kWaves * 16 * RT * D * 4 <= kLds, "the sums of all waves fit (add_odd)");
 };
 
@@ -58,15 +58,13 @@ void pages_chunk_kernel(AttendArgs a) {
   using G = Chunk<D, Q8, RT>;
   constexpr int kRowBytes = G::kRowBytes, kTileBytes = G::kTileBytes, NSL = G::kSlabs, NCB = G::kBlocks;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ long long row_at[G::kRows];                  // byte offset of each output row, -1: none
-  __shared__ int row_end[G::kRows], row_begin[G::kRows];  // what each row sees
-  __shared__ int any_odd;                                 // values that are not finite have been taken out of a tile
   const PagesView& c = a.c;
 
-  const int wg = xcd_order(SCALEKV_WG_X, a.n_wg);  // row groups of a unit share an L2
-  const int split = wg % a.n_split, unit = wg / a.n_split / a.n_row_group;
+  int unit, part_of;
+  unit_of(SCALEKV_WG_X, a.n_wg, a.n_split * a.n_row_group, unit, part_of);
   // under a causal mask later rows see more: they come first, so that the short ones fill up the end
-  const int nth = wg / a.n_split % a.n_row_group, row_group = a.mask.causal ? a.n_row_group - 1 - nth : nth;
+  const int split = part_of % a.n_split, nth = part_of / a.n_split;
+  const int row_group = a.mask.causal ? a.n_row_group - 1 - nth : nth;
   const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -89,15 +87,7 @@ void pages_chunk_kernel(AttendArgs a) {
     const bool there = at >= 0 && at < a.q.n_row;
 #pragma unroll
     for (int sl = 0; sl < NSL; ++sl) qf[b][sl] = __builtin_bit_cast(bf16x8, there ? src[4 * sl + g] : u32x4{0, 0, 0, 0});
-    if (g == 0) {
-      const int slot = 16 * (RT * wave + b) + i;
-      const bool store = wave_row + 16 * b + i < seen.n_rows && at >= 0 && at < a.out.n_row;
-      row_at[slot] = store ? seq * a.out.seq + head * a.out.head + at * a.out.row : -1;
-      row_end[slot] = seen.end_of(seen.pos0 + t);
-      row_begin[slot] = seen.begin_of(seen.pos0 + t);
-    }
   }
-  if (tid == 0) any_odd = 0;
 
   // ---- tiles
   auto lds_addr = [](const unsigned char* p) -> unsigned {
@@ -105,6 +95,8 @@ void pages_chunk_kernel(AttendArgs a) {
   };
   unsigned char* const k_lds = smem;
   unsigned char* const v_lds = smem + 2 * kTileBytes;
+  unsigned char* const raw_lds = smem + 4 * kTileBytes;  // e4m3: the codes of the next tiles, K's and V's, wave by wave
+  bool odd = false;  // this wave has taken values that are not finite out of a tile
   const int32_t* const table = c.table + (long long)seq * c.width;
   const long long kv_ofs = kv * c.head;
   auto key0_of = [&](int t) { return seen.key0(t0 + t); };
@@ -146,59 +138,72 @@ void pages_chunk_kernel(AttendArgs a) {
       }
     }
   };
-  // e4m3: a lane has kVecs vectors of 16 codes; vector p lies in row 16 wave + (16 / kVecs) p + lane / (D / 16)
-  constexpr int kSrcChunks = D / 16, kVecRows = 16 / G::kVecs;
-  const int q8_row = lane / kSrcChunks, q8_chunk = lane % kSrcChunks;
-  u32x4 k_raw[G::kVecs], v_raw[G::kVecs];
+  // e4m3: the codes of 16 rows, as they lie in the page; a lane widens kVecs vectors of 16 codes, vector p of row
+  // kVecRows p + lane / kSrcChunks of those
+  constexpr int kSrcChunks = D / 16, kVecRows = 16 / G::kVecs, kRawBytes = 16 * D;
+  const int q8_row = lane / kSrcChunks;
+  const unsigned raw_k = __builtin_amdgcn_readfirstlane(lds_addr(raw_lds + wave * kRawBytes));
+  const unsigned raw_v = raw_k + kWaves * kRawBytes;
   uint8_t k_sc[G::kVecs], v_sc[G::kVecs];
-  auto fetch = [&](const unsigned char* pool, const uint8_t* scales, int page, int t, u32x4 (&raw)[G::kVecs],
+  auto fetch = [&](const unsigned char* pool, const uint8_t* scales, int page, int t, unsigned dst,
                    uint8_t (&sc)[G::kVecs]) __attribute__((always_inline)) {
     const int pos = key0_of(t) + 16 * wave, slot = pos & ((1 << c.page_shift) - 1);
-    const bool in_pool = (unsigned)page < (unsigned)c.n_page;
     const unsigned char* rows = rows_at(pool, page, t);
-    const uint8_t* scale = in_pool ? scales + page * c.scale_page + kv * c.scale_head + slot : (const uint8_t*)g_zero_rows;
+    const unsigned char* scale = scalar((unsigned)page < (unsigned)c.n_page
+                                            ? scales + page * c.scale_page + kv * c.scale_head + slot
+                                            : g_zero_rows);
 #pragma unroll
-    for (int p = 0; p < G::kVecs; ++p) {
-      raw[p] = *(const u32x4*)(rows + 1024 * p + 16 * lane);
-      sc[p] = scale[kVecRows * p + q8_row];
-      if (!seen.every(pos, 16) && !seen.some(pos + kVecRows * p + q8_row)) raw[p] = u32x4{0, 0, 0, 0};
+    for (int p = 0; p < G::kVecs; ++p) sc[p] = scale[kVecRows * p + q8_row];
+    if (seen.every(pos, 16)) {
+      dma16<0>(rows, 16 * lane, dst);
+      if constexpr (G::kVecs == 2) dma16<1024>(rows, 16 * lane, dst);
+    } else {
+#pragma unroll
+      for (int p = 0; p < G::kVecs; ++p) {
+        const bool there = seen.some(pos + kVecRows * p + q8_row);
+        dma16_lane((there ? rows : (const unsigned char*)g_zero_rows) + 1024 * p + 16 * lane, dst + 1024 * p);
+      }
     }
   };
-  auto put = [&](unsigned char* stage, const u32x4 (&raw)[G::kVecs], const uint8_t (&sc)[G::kVecs], bool values, bool edge)
+  auto put = [&](unsigned char* stage, const unsigned char* raw, const uint8_t (&sc)[G::kVecs], bool values, bool edge)
                  __attribute__((always_inline)) {
+    // (addresses are formed on the spot: held through the tile loop they are spilled)
+    int ld = lane;
+    asm volatile("" : "+v"(ld));
 #pragma unroll
     for (int p = 0; p < G::kVecs; ++p) {
-      const int row = 16 * wave + kVecRows * p + q8_row;
+      const int row = 16 * wave + kVecRows * p + ld / kSrcChunks;
       u32x4 x[2];
-      widen(raw[p], __uint_as_float((unsigned)sc[p] << 23), x);
-      if (values && edge && (take_odd<true>(x[0]) | take_odd<true>(x[1]))) any_odd = 1;
+      widen(*(const u32x4*)(raw + 1024 * p + 16 * ld), __uint_as_float((unsigned)sc[p] << 23), x);
+      if (values && edge) odd |= __builtin_amdgcn_ballot_w64(take_odd<true>(x[0]) | take_odd<true>(x[1])) != 0;
       const int flip = values ? v_flip_bf16<D>(row) : k_flip_bf16<D>(row);
 #pragma unroll
-      for (int w = 0; w < 2; ++w) *(u32x4*)(stage + row * kRowBytes + 16 * ((2 * q8_chunk + w) ^ flip)) = x[w];
+      for (int w = 0; w < 2; ++w) *(u32x4*)(stage + row * kRowBytes + 16 * ((2 * (ld % kSrcChunks) + w) ^ flip)) = x[w];
       __builtin_amdgcn_sched_barrier(0);  // (a vector at a time: registers are scarce here)
     }
   };
   auto issue_k = [&](int t, int page) __attribute__((always_inline)) {
-    if constexpr (Q8) fetch(c.k, c.k_scale, page, t, k_raw, k_sc);
+    if constexpr (Q8) fetch(c.k, c.k_scale, page, t, raw_k, k_sc);
     else
       transfer(rows_at(c.k, page, t), t, k_wave + (t & 1) * kTileBytes,
                [&](int p) { return ld_k + (ld_kchunk ^ k_step(p)); });
   };
   auto issue_v = [&](int t, int page) __attribute__((always_inline)) {
-    if constexpr (Q8) fetch(c.v, c.v_scale, page, t, v_raw, v_sc);
+    if constexpr (Q8) fetch(c.v, c.v_scale, page, t, raw_v, v_sc);
     else transfer(rows_at(c.v, page, t), t, v_wave + (t & 1) * kTileBytes, [&](int) { return ld_v; });
   };
-  auto put_k = [&](int t) { put(k_lds + (t & 1) * kTileBytes, k_raw, k_sc, false, false); };
-  auto put_v = [&](int t) { put(v_lds + (t & 1) * kTileBytes, v_raw, v_sc, true, seen.edge(t0 + t)); };
+  auto put_k = [&](int t) { put(k_lds + (t & 1) * kTileBytes, raw_lds + wave * kRawBytes, k_sc, false, false); };
+  auto put_v = [&](int t) {
+    put(v_lds + (t & 1) * kTileBytes, raw_lds + (kWaves + wave) * kRawBytes, v_sc, true, seen.edge(t0 + t));
+  };
   // bf16: values of an edge tile that are not finite, in the rows that this wave has brought in
   auto sift = [&](int t) {
     unsigned char* const mine = v_lds + (t & 1) * kTileBytes + 16 * wave * kRowBytes + 16 * lane;
     for (int p = 0; p < G::kOps; ++p) {
       u32x4 x = *(const u32x4*)(mine + 1024 * p);
-      if (take_odd<true>(x)) {
-        *(u32x4*)(mine + 1024 * p) = x;
-        any_odd = 1;
-      }
+      const bool found = take_odd<true>(x);
+      if (found) *(u32x4*)(mine + 1024 * p) = x;
+      odd |= __builtin_amdgcn_ballot_w64(found) != 0;
     }
   };
 
@@ -290,7 +295,8 @@ void pages_chunk_kernel(AttendArgs a) {
       const int pos0 = key0 + 32 * h + 16 * (mine >> 4 & 1) + 8 * (mine >> 5);
 #pragma unroll
       for (int b = 0; b < RT; ++b) {
-        const int end = row_end[16 * (RT * wave + b) + (mine & 15)], begin = row_begin[16 * (RT * wave + b) + (mine & 15)];
+        const int p = seen.pos0 + min(wave_row + 16 * b + (mine & 15), seen.n_rows - 1) / a.group;
+        const int end = seen.end_of(p), begin = seen.begin_of(p);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const int pos = pos0 + x;
@@ -341,10 +347,11 @@ void pages_chunk_kernel(AttendArgs a) {
   // have left.
   auto turn = [&](int t) __attribute__((always_inline)) {
     if constexpr (Q8) {
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what this wave has put is there
+      __builtin_amdgcn_s_waitcnt(0);  // what this wave has asked for and put is there
       __syncthreads();
       if (t + 1 < n_tile) put_v(t + 1);
       if (t + 2 < n_tile) put_k(t + 2);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the codes are read, their places may be filled again
       if (t + 2 < n_tile) issue_v(t + 2, page_k);
       const int page = __builtin_amdgcn_readfirstlane(page_next);
       if (t + 3 < n_tile) issue_k(t + 3, page);
@@ -403,22 +410,24 @@ void pages_chunk_kernel(AttendArgs a) {
   if (n_tile > 0) {
     {
       const int p0 = __builtin_amdgcn_readfirstlane(ask_page(0)), p1 = __builtin_amdgcn_readfirstlane(ask_page(1));
-      __syncthreads();  // (any_odd and the rows' tables are written)
       if constexpr (Q8) {
         const int p2 = __builtin_amdgcn_readfirstlane(ask_page(2));
         issue_k(0, p0);
         issue_v(0, p0);
+        __builtin_amdgcn_s_waitcnt(0);
         put_k(0);
         put_v(0);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
         if (n_tile > 1) {
           issue_k(1, p1);
-          put_k(1);
           issue_v(1, p1);
+          __builtin_amdgcn_s_waitcnt(0);
+          put_k(1);
+          __builtin_amdgcn_s_waitcnt(0xc07f);
         }
         if (n_tile > 2) issue_k(2, p2);
         page_k = p2;
         page_next = ask_page(3);
-        __builtin_amdgcn_s_waitcnt(0xc07f);
       } else {
         issue_k(0, p0);
         issue_v(0, p0);
@@ -474,10 +483,17 @@ void pages_chunk_kernel(AttendArgs a) {
     }
   }
   __syncthreads();  // all waves have left the tiles
+  bool any_odd = false;
+  if (a.mask.causal || seen.window) {  // (without a mask no row sees what another does not)
+    if (lane == 0) ((int*)smem)[wave] = odd;
+    __syncthreads();
+    for (int x = 0; x < kWaves; ++x) any_odd |= ((const int*)smem)[x] != 0;
+    __syncthreads();
+  }
   if (wave_row >= seen.n_rows) return;
   // (each wave has a part of the LDS to itself from here on, for add_odd() and then for its output)
   unsigned char* const mine = smem + wave * (16 * RT * D * 4);
-  if (n_tile > 0 && any_odd) {
+  if (any_odd) {
     float* const sums = (float*)mine;
     sums_to_lds<D, RT>(o, sums);
     add_odd<kTypeBf16, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t0 + n_tile, 0, TN, neg, sums);
@@ -525,8 +541,10 @@ void pages_chunk_kernel(AttendArgs a) {
   for (int p = 0; p < 16 * RT / G::kRowsPerOp; ++p) {
     const int r = G::kRowsPerOp * p + lane / G::kChunks;
     const u32x4 val = *(const u32x4*)(mine + r * kOutStride + 16 * (lane % G::kChunks));
-    const long long at = row_at[16 * RT * wave + r];
-    if (at >= 0) *(u32x4*)(a.out.p + at + 16 * (lane % G::kChunks)) = val;
+    const int nth_row = wave_row + r, t = nth_row / a.group, head = kv * a.group + (nth_row - t * a.group);
+    const long long at = (long long)chunk_first(a.chunk, seq) + t;
+    if (nth_row < seen.n_rows && at >= 0 && at < a.out.n_row)
+      *(u32x4*)(a.out.p + (seq * a.out.seq + head * a.out.head + at * a.out.row) + 16 * (lane % G::kChunks)) = val;
   }
 }
 
