@@ -48,6 +48,7 @@ struct Seen {
   bool window;
   int causal, width;             // of the mask
   int sink_tiles, from_tile, n_tile;
+  int plain_begin, plain_end;    // every row sees all of these tiles
   __device__ __forceinline__ int end_of(int p) const { return causal ? min(len, p + 1) : len; }
   __device__ __forceinline__ int begin_of(int p) const { return window ? p - width + 1 : -0x7fffffff; }
   __device__ __forceinline__ Seen(const AttendArgs& a, int seq, int first_row, int rows) {
@@ -68,7 +69,10 @@ struct Seen {
     sink_tiles = (max(min(sinks, hi), 0) + TN - 1) / TN;
     from_tile = max(max(lo, 0) / TN, sink_tiles);
     n_tile = sink_tiles + max((hi + TN - 1) / TN - from_tile, 0);
+    plain_begin = window ? sink_tiles + max((max(all_begin, 0) + TN - 1) / TN - from_tile, 0) : 0;
+    plain_end = sink_tiles + max(all_end, 0) / TN - from_tile;
   }
+  __device__ __forceinline__ bool plain(int t) const { return t >= plain_begin && t < plain_end; }
   __device__ __forceinline__ int key0(int t) const { return (t < sink_tiles ? t : from_tile + t - sink_tiles) * TN; }
   // does some row see this position; any of [pos, pos + n); all of them
   __device__ __forceinline__ bool some(int pos) const { return pos < hi && (pos >= lo || pos < sinks); }

@@ -103,7 +103,7 @@ void pages_chunk_kernel(AttendArgs a) {
   // the page of this wave's rows of tile t; any number outside the pool stands for rows of zeros
   auto ask_page = [&](int t) -> int {
     const int pos = key0_of(t) + 16 * wave;
-    return t < n_tile && seen.any(pos, 16) ? table[pos >> c.page_shift] : -1;
+    return t < n_tile && (seen.plain(t0 + t) || seen.any(pos, 16)) ? table[pos >> c.page_shift] : -1;
   };
   int page_next = -1;  // of the tile whose K rows are requested next (as it was loaded; made a scalar when it is used)
   int page_k = -1;     // of the tile before: its V rows are requested with them
@@ -122,7 +122,7 @@ void pages_chunk_kernel(AttendArgs a) {
   const unsigned k_wave = __builtin_amdgcn_readfirstlane(lds_addr(k_lds + 16 * wave * kRowBytes));
   const unsigned v_wave = __builtin_amdgcn_readfirstlane(lds_addr(v_lds + 16 * wave * kRowBytes));
   auto transfer = [&](const unsigned char* rows, int t, unsigned dst, auto ofs) __attribute__((always_inline)) {
-    if (seen.every(key0_of(t) + 16 * wave, 16)) {
+    if (seen.plain(t0 + t) || seen.every(key0_of(t) + 16 * wave, 16)) {
       // (the immediate offset moves the destination along with the source)
       dma16<0>(rows, ofs(0), dst);
       dma16<1024>(rows, ofs(1), dst);
@@ -154,7 +154,7 @@ void pages_chunk_kernel(AttendArgs a) {
                                             : g_zero_rows);
 #pragma unroll
     for (int p = 0; p < G::kVecs; ++p) sc[p] = scale[kVecRows * p + q8_row];
-    if (seen.every(pos, 16)) {
+    if (seen.plain(t0 + t) || seen.every(pos, 16)) {
       dma16<0>(rows, 16 * lane, dst);
       if constexpr (G::kVecs == 2) dma16<1024>(rows, 16 * lane, dst);
     } else {
@@ -165,23 +165,24 @@ void pages_chunk_kernel(AttendArgs a) {
       }
     }
   };
-  auto put = [&](unsigned char* stage, const unsigned char* raw, const uint8_t (&sc)[G::kVecs], bool values, bool edge)
+  // Vector p of them into the tile, in two steps: load() and put()
+  u32x4 raw;
+  auto load = [&](const unsigned char* codes, int p) { raw = *(const u32x4*)(codes + 1024 * p + 16 * lane); };
+  auto put = [&](unsigned char* stage, const uint8_t (&sc)[G::kVecs], int p, bool values, bool edge)
                  __attribute__((always_inline)) {
     // (addresses are formed on the spot: held through the tile loop they are spilled)
     int ld = lane;
     asm volatile("" : "+v"(ld));
+    const int row = 16 * wave + kVecRows * p + ld / kSrcChunks;
+    u32x4 x[2];
+    widen(raw, __uint_as_float((unsigned)sc[p] << 23), x);
+    if (values && edge) odd |= __builtin_amdgcn_ballot_w64(take_odd<true>(x[0]) | take_odd<true>(x[1])) != 0;
+    const int flip = values ? v_flip_bf16<D>(row) : k_flip_bf16<D>(row);
 #pragma unroll
-    for (int p = 0; p < G::kVecs; ++p) {
-      const int row = 16 * wave + kVecRows * p + ld / kSrcChunks;
-      u32x4 x[2];
-      widen(*(const u32x4*)(raw + 1024 * p + 16 * ld), __uint_as_float((unsigned)sc[p] << 23), x);
-      if (values && edge) odd |= __builtin_amdgcn_ballot_w64(take_odd<true>(x[0]) | take_odd<true>(x[1])) != 0;
-      const int flip = values ? v_flip_bf16<D>(row) : k_flip_bf16<D>(row);
-#pragma unroll
-      for (int w = 0; w < 2; ++w) *(u32x4*)(stage + row * kRowBytes + 16 * ((2 * (ld % kSrcChunks) + w) ^ flip)) = x[w];
-      __builtin_amdgcn_sched_barrier(0);  // (a vector at a time: registers are scarce here)
-    }
+    for (int w = 0; w < 2; ++w) *(u32x4*)(stage + row * kRowBytes + 16 * ((2 * (ld % kSrcChunks) + w) ^ flip)) = x[w];
   };
+  unsigned char* const k_codes = raw_lds + wave * kRawBytes;
+  unsigned char* const v_codes = raw_lds + (kWaves + wave) * kRawBytes;
   auto issue_k = [&](int t, int page) __attribute__((always_inline)) {
     if constexpr (Q8) fetch(c.k, c.k_scale, page, t, raw_k, k_sc);
     else
@@ -192,9 +193,28 @@ void pages_chunk_kernel(AttendArgs a) {
     if constexpr (Q8) fetch(c.v, c.v_scale, page, t, raw_v, v_sc);
     else transfer(rows_at(c.v, page, t), t, v_wave + (t & 1) * kTileBytes, [&](int) { return ld_v; });
   };
-  auto put_k = [&](int t) { put(k_lds + (t & 1) * kTileBytes, raw_lds + wave * kRawBytes, k_sc, false, false); };
-  auto put_v = [&](int t) {
-    put(v_lds + (t & 1) * kTileBytes, raw_lds + (kWaves + wave) * kRawBytes, v_sc, true, seen.edge(t0 + t));
+  auto put_v = [&](int t, int p) __attribute__((always_inline)) {
+    put(v_lds + (t & 1) * kTileBytes, v_sc, p, true, !seen.plain(t0 + t) && seen.edge(t0 + t));
+  };
+  auto put_k = [&](int t, int p) __attribute__((always_inline)) { put(k_lds + (t & 1) * kTileBytes, k_sc, p, false, false); };
+  // Between turn(t) and the next: V of tile t + 1 and K of tile t + 2, whose codes have arrived, into the tile; step e of
+  // 4 kVecs.  Then the codes behind them are asked for.
+  auto widen_step = [&](int t, int e) __attribute__((always_inline)) {
+    const int p = e / 2 % G::kVecs;
+    const bool values = e / 2 < G::kVecs;
+    if (values ? t + 1 >= n_tile : t + 2 >= n_tile) return;
+    if (e % 2 == 0) load(values ? v_codes : k_codes, p);
+    else if (values) put_v(t + 1, p);
+    else put_k(t + 2, p);
+  };
+  auto ask_codes = [&](int t) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the codes are read, their places may be filled again
+    if (t + 2 < n_tile) issue_v(t + 2, page_k);
+    const int page = __builtin_amdgcn_readfirstlane(page_next);
+    if (t + 3 < n_tile) issue_k(t + 3, page);
+    page_k = page;
+    page_next = ask_page(t + 4);
+    __builtin_amdgcn_sched_barrier(0);
   };
   // bf16: values of an edge tile that are not finite, in the rows that this wave has brought in
   auto sift = [&](int t) {
@@ -290,7 +310,7 @@ void pages_chunk_kernel(AttendArgs a) {
   // Before the softmax of a block (half h of tile t): hide what its rows do not see, and move the offsets if need be.
   auto prepare = [&](f32x4 (&s)[RT][2], int t, int h) __attribute__((always_inline)) {
     const int key0 = key0_of(t);
-    if (key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > seen.sinks)) {
+    if (!seen.plain(t0 + t) && (key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > seen.sinks))) {
       const int mine = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
       const int pos0 = key0 + 32 * h + 16 * (mine >> 4 & 1) + 8 * (mine >> 5);
 #pragma unroll
@@ -327,6 +347,7 @@ void pages_chunk_kernel(AttendArgs a) {
   };
   auto rescale = [&]() __attribute__((always_inline)) {
     if (moved) {
+      asm volatile("");  // (a branch: the products of all accumulators are not to be formed and thrown away)
 #pragma unroll
       for (int b = 0; b < RT; ++b)
 #pragma unroll
@@ -349,17 +370,9 @@ void pages_chunk_kernel(AttendArgs a) {
     if constexpr (Q8) {
       __builtin_amdgcn_s_waitcnt(0);  // what this wave has asked for and put is there
       __syncthreads();
-      if (t + 1 < n_tile) put_v(t + 1);
-      if (t + 2 < n_tile) put_k(t + 2);
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the codes are read, their places may be filled again
-      if (t + 2 < n_tile) issue_v(t + 2, page_k);
-      const int page = __builtin_amdgcn_readfirstlane(page_next);
-      if (t + 3 < n_tile) issue_k(t + 3, page);
-      page_k = page;
-      page_next = ask_page(t + 4);
     } else {
       __builtin_amdgcn_s_waitcnt(0);
-      if (seen.edge(t0 + t)) {
+      if (!seen.plain(t0 + t) && seen.edge(t0 + t)) {
         sift(t);
         __builtin_amdgcn_s_waitcnt(0xc07f);
       }
@@ -400,8 +413,15 @@ void pages_chunk_kernel(AttendArgs a) {
           [&](int m) {
 #pragma unroll
             for (int e = m * kVReads / kSlots; e < (m + 1) * kVReads / kSlots; ++e) read_v(st * kTileBytes, e);
+            if constexpr (Q8) {
+              // a vector is asked for in one slot and put some slots later
+              constexpr int kApart = kSlots / (2 * G::kVecs);
+              if (m % kApart == 0) widen_step(t, m / kApart * 2);
+              if (m % kApart == kApart - 1) widen_step(t, m / kApart * 2 + 1);
+            }
           },
           sb, pb, 0);
+    if constexpr (Q8) ask_codes(t);
     slots([&](int m) { value_mfma(pa, m); },
           [&](int m) { if (m < kKReads) read_k((st ^ 1) * kTileBytes + kHalf, m); }, sb, pb, 8 * RT);
     rescale();
@@ -415,14 +435,14 @@ void pages_chunk_kernel(AttendArgs a) {
         issue_k(0, p0);
         issue_v(0, p0);
         __builtin_amdgcn_s_waitcnt(0);
-        put_k(0);
-        put_v(0);
+        for (int p = 0; p < G::kVecs; ++p) load(k_codes, p), put_k(0, p);
+        for (int p = 0; p < G::kVecs; ++p) load(v_codes, p), put_v(0, p);
         __builtin_amdgcn_s_waitcnt(0xc07f);
         if (n_tile > 1) {
           issue_k(1, p1);
           issue_v(1, p1);
           __builtin_amdgcn_s_waitcnt(0);
-          put_k(1);
+          for (int p = 0; p < G::kVecs; ++p) load(k_codes, p), put_k(1, p);
           __builtin_amdgcn_s_waitcnt(0xc07f);
         }
         if (n_tile > 2) issue_k(2, p2);
@@ -479,7 +499,13 @@ void pages_chunk_kernel(AttendArgs a) {
 #pragma unroll
       for (int m = 0; m < kSlots; ++m) value_mfma(pb, m);
     } else {
-      for (int t = 0; t < n_tile; ++t) turn(t);  // (a wave without rows only carries its share of the tiles)
+      for (int t = 0; t < n_tile; ++t) {  // (a wave without rows only carries its share of the tiles)
+        turn(t);
+        if constexpr (Q8) {
+          for (int e = 0; e < 4 * G::kVecs; ++e) widen_step(t, e);
+          ask_codes(t);
+        }
+      }
     }
   }
   __syncthreads();  // all waves have left the tiles
