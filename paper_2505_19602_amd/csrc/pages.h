@@ -54,18 +54,25 @@ hipError_t launch_pages_write(int dtype, int d, int n_seq, const PagesView& page
 hipError_t launch_pages_read(int dtype, int d, int n_seq, int n_head, const PagesView& pages, const int32_t* idx, int n_row,
                              KvView k_dst, KvView v_dst, hipStream_t stream);
 
-// How scalekv_pages_attend cuts its work.  A workgroup has the query rows (token, query head) of one KV head, so that
-// they share its rows of the cache.
+// How scalekv_pages_attend cuts its work.  A workgroup has query rows (token, query head) of one KV head, so that they
+// share its rows of the cache.
 struct PagesPlan {
-  int row_waves;   // waves of a workgroup that split its query rows; the others split the keys of a tile
-  int row_tiles;   // tiles of 16 query rows to a wave
-  int n_row_group; // workgroups to the query rows of a unit
-  int n_split;     // workgroups to the keys of a row group; their results are joined by a launch of its own
+  int row_waves;     // waves of a workgroup that split its query rows; the others split the keys of a tile
+  int row_tiles;     // tiles of 16 query rows to a wave
+  int target;        // workgroups that the keys are to be cut for, where that takes more than the rows do; 0: never
+  int min_tiles;     // tiles that a workgroup has at least, where keys are cut
+  int n_wg;          // workgroups of the launch: as many as there may be
   int rows() const { return 16 * row_waves * row_tiles; }
 };
 PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& pages, int max_new, const MaskView& mask);
-inline size_t pages_partial_bytes(int n_seq, int n_head, int d, int max_new, const PagesPlan& plan) {
-  return plan.n_split < 2 ? 0 : (size_t)n_seq * n_head * max_new * plan.n_split * (d + 2) * sizeof(float);
+// Workspace: the sums of every workgroup's rows, {offset, sum of weights} of each, {first workgroup, cuts} of each sequence.
+inline size_t pages_partial_rows(int group, int max_new, const PagesPlan& plan) {
+  const long long unit_rows = (long long)group * max_new;
+  return (size_t)plan.n_wg * (size_t)(unit_rows < plan.rows() ? unit_rows : plan.rows());
+}
+inline size_t pages_partial_bytes(int n_seq, int d, int group, int max_new, const PagesPlan& plan) {
+  if (plan.target == 0) return 0;
+  return pages_partial_rows(group, max_new, plan) * (size_t)(d + 2) * sizeof(float) + (size_t)n_seq * 2 * sizeof(int);
 }
 hipError_t launch_pages_attend(int dtype, int d, int n_seq, int n_head, const PagesView& pages, const RowsView& q,
                                const RowsView& out, const ChunkView& chunk, const MaskView& mask, float sm_scale,

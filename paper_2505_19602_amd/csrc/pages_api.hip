@@ -184,8 +184,7 @@ scalekv_status check_mask(const scalekv_mask* m, MaskView* out) {
 // the plan of an attention whose arguments have passed the checks
 scalekv_status make_plan(const scalekv_shape* s, const scalekv_pages* c, int max_new, const MaskView& mask, PagesPlan* plan) {
   *plan = pages_plan(s->dtype, s->head_dim, s->n_seq, s->n_head, pages_view(s, c), max_new, mask);
-  const long long n_wg = (long long)s->n_seq * c->n_kv_head * plan->n_row_group * plan->n_split;
-  if (n_wg > 0x7fffffffLL) return fail(SCALEKV_ERR_UNSUPPORTED, "this call needs %lld workgroups", n_wg);
+  if (plan->n_wg < 0) return fail(SCALEKV_ERR_UNSUPPORTED, "this call needs more than 2^31 - 1 workgroups");
   return SCALEKV_OK;
 }
 
@@ -255,7 +254,7 @@ scalekv_status scalekv_pages_workspace_bytes(const scalekv_shape* shape, const s
   SCALEKV_TRY(check_mask(mask, &m));
   PagesPlan plan;
   SCALEKV_TRY(make_plan(shape, pages, max_new, m, &plan));
-  *out = pages_partial_bytes(shape->n_seq, shape->n_head, shape->head_dim, max_new, plan);
+  *out = pages_partial_bytes(shape->n_seq, shape->head_dim, shape->n_head / pages->n_kv_head, max_new, plan);
   return SCALEKV_OK;
 }
 
@@ -280,7 +279,8 @@ scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pa
   if (meets_pool(shape, pages, o)) return fail(SCALEKV_ERR_INVALID_ARG, "out overlaps the pool");
   PagesPlan plan;
   SCALEKV_TRY(make_plan(shape, pages, chunk->max_new, m, &plan));
-  const size_t need = pages_partial_bytes(shape->n_seq, shape->n_head, shape->head_dim, chunk->max_new, plan);
+  const size_t need =
+      pages_partial_bytes(shape->n_seq, shape->head_dim, shape->n_head / pages->n_kv_head, chunk->max_new, plan);
   if (need > 0) {
     if (!ws) return fail(SCALEKV_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
     if (!aligned16(ws)) return fail(SCALEKV_ERR_INVALID_ARG, "workspace is not 16-byte aligned");

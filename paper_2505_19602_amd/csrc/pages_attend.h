@@ -15,27 +15,137 @@ struct AttendArgs {
   RowsView q, out;
   ChunkView chunk;
   MaskView mask;
-  int n_seq, group, n_row_group, n_split, n_wg;
+  int n_seq, group, rows, target, min_tiles;
   float scale_log2e, no_max;
-  float *part, *stat;  // partial sums [row][split][D], their {largest logit in log2 units, sum} [row][split][2]
+  // workspace (target > 0): sums [workgroup][part_rows][D], their {offset in log2 units, sum of weights}, {first workgroup,
+  // cuts} of each sequence
+  float *part, *stat;
+  int2* cuts;
+  int part_rows;
 };
 
 // bf16, many query rows (pages_chunk.hip): 64 row_tiles rows to a workgroup
-hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, hipStream_t stream);
+hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, int n_wg, hipStream_t stream);
 
-// Which unit a workgroup works on, and which part of it: units are dealt out to the XCDs in turn (consecutive workgroup ids go
-// round-robin over them), so that the workgroups of a unit share an L2 and the units of a long sequence do not.
-__device__ __forceinline__ void unit_of(int wg, int n_wg, int per_unit, int& unit, int& part) {
-  const int dealt = n_wg / per_unit / kXcds * kXcds;  // units of whole rounds; the rest one behind the other
-  if (wg < dealt * per_unit) {
-    const int nth = wg / kXcds;
-    unit = nth / per_unit * kXcds + wg % kXcds;
-    part = nth % per_unit;
-  } else {
-    const int rest = wg - dealt * per_unit;
-    unit = dealt + rest / per_unit;
-    part = rest % per_unit;
+// Sum over the lanes of a wave, in all of them; sum over the lanes up to one's own.  (DPP: shifts within rows of 16 lanes,
+// then the last lane of a row, and of the lower half, to those behind it.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp_add(unsigned x) {
+  return x + (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ unsigned wave_scan(unsigned x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double x) {
+  const unsigned long long bits = __builtin_bit_cast(unsigned long long, x);
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)bits, CTRL, ROWS, 0xf, false);
+  const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(bits >> 32), CTRL, ROWS, 0xf, false);
+  return x + __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  x = dpp_add<0x143, 0xc>(x);
+  const unsigned long long bits = __builtin_bit_cast(unsigned long long, x);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)bits, 63), hi = __builtin_amdgcn_readlane((int)(unsigned)(bits >> 32), 63);
+  return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+
+// What a workgroup works on.  The lengths of the sequences are known to the device alone, and may differ by any factor: every
+// workgroup adds up the work of all of them (tiles times row groups) and finds its own place.  A sequence's
+// keys are cut into as many parts as it has multiples of `most` tiles, the work of all sequences over `target` workgroups
+// (and at least min_tiles), so that a long sequence does not outlast the others, and short ones are not cut.
+struct Slice {
+  int seq, kv, row_group, cut, cuts;  // cuts 0: nothing
+  int first_wg;                       // of the sequence
+};
+struct Cutter {
+  const AttendArgs& a;
+  int tile;   // keys of a tile
+  int most;   // tiles to a workgroup
+  __device__ __forceinline__ int groups(int seq) const {
+    return (chunk_count(a.chunk, seq) * a.group + a.rows - 1) / a.rows;
   }
+  __device__ __forceinline__ int tiles(int seq) const {
+    const int all = (pages_len(a.c, seq) + tile - 1) / tile;
+    if (a.mask.window == 0 || !a.mask.causal) return all;
+    const int tokens = min(a.chunk.max_new, a.rows / a.group + 1);
+    return min(all, (min(a.mask.n_sink, 1 << 29) + tile - 1) / tile + (min(a.mask.window, 1 << 29) + tokens) / tile + 1);
+  }
+  __device__ __forceinline__ int cuts(int seq) const { return a.target ? max((tiles(seq) + most - 1) / most, 1) : 1; }
+  __device__ __forceinline__ unsigned workgroups(int seq) const { return (unsigned)(groups(seq) * cuts(seq)) * a.c.n_kv_head; }
+};
+template <int TN>
+__device__ __forceinline__ Slice slice_of(const AttendArgs& a, unsigned wg) {
+  Cutter cutter{a, TN, 1};
+  const int lane = threadIdx.x & 63, per_lane = (a.n_seq + 63) / 64;
+  Slice s{};
+  unsigned first = 0;
+  if (a.n_seq == 1) {
+    if (a.target) {
+      const double work = (double)cutter.groups(0) * cutter.tiles(0) * a.c.n_kv_head;
+      cutter.most = max(a.min_tiles, (int)min(ceil(work / a.target), 1e9));
+    }
+    if (wg >= cutter.workgroups(0)) return s;
+  } else {
+    if (a.target) {
+      double work = 0;
+      for (int x = lane * per_lane; x < min((lane + 1) * per_lane, a.n_seq); ++x)
+        work += (double)cutter.groups(x) * cutter.tiles(x);
+      cutter.most = max(a.min_tiles, (int)min(ceil(wave_sum(work) * a.c.n_kv_head / a.target), 1e9));
+    }
+    unsigned mine = 0;
+    for (int x = lane * per_lane; x < min((lane + 1) * per_lane, a.n_seq); ++x) mine += cutter.workgroups(x);
+    const unsigned upto = wave_scan(mine);
+    const unsigned long long found = __builtin_amdgcn_ballot_w64(upto > wg);  // this lane's sequences or earlier ones
+    if (found == 0) return s;
+    const int at = __builtin_ctzll(found);
+    first = __builtin_amdgcn_readlane((int)(upto - mine), at);
+    s.seq = at * per_lane;
+    for (unsigned n; wg >= first + (n = cutter.workgroups(s.seq)); ++s.seq) first += n;
+    s.seq = __builtin_amdgcn_readfirstlane(s.seq);
+    first = __builtin_amdgcn_readfirstlane(first);
+  }
+  s.first_wg = (int)first;
+  s.cuts = __builtin_amdgcn_readfirstlane(cutter.cuts(s.seq));
+  const int n_group = __builtin_amdgcn_readfirstlane(cutter.groups(s.seq)), per = n_group * s.cuts;
+  // Eight heads at a time, dealt out in turn: consecutive workgroups go round-robin over the XCDs, so that the workgroups
+  // of a head share an L2.
+  const int heads = a.c.n_kv_head, dealt = heads / kXcds * kXcds;
+  int j = (int)(wg - first), rest;
+  if (j < dealt * per) {
+    const int round = j / (kXcds * per);
+    j -= round * kXcds * per;
+    s.kv = round * kXcds + j % kXcds;
+    rest = j / kXcds;
+  } else {
+    j -= dealt * per;
+    s.kv = dealt + j % (heads - dealt);
+    rest = j / (heads - dealt);
+  }
+  s.cut = rest % s.cuts;
+  // under a causal mask later rows see more: they come first, so that the short ones fill up the end
+  const int nth = rest / s.cuts;
+  s.row_group = a.mask.causal ? n_group - 1 - nth : nth;
+  if (a.target && wg == first && threadIdx.x == 0) a.cuts[s.seq] = make_int2(s.first_wg, s.cuts);
+  return s;
+}
+// The workgroup of a part, from what slice_of() has left in the workspace: its inverse.
+__device__ __forceinline__ int workgroup_of(const AttendArgs& a, int first_wg, int cuts, int n_group, int kv, int row_group,
+                                            int cut) {
+  const int heads = a.c.n_kv_head, dealt = heads / kXcds * kXcds, per = n_group * cuts;
+  const int rest = (a.mask.causal ? n_group - 1 - row_group : row_group) * cuts + cut;
+  return first_wg + (kv < dealt ? kv / kXcds * (kXcds * per) + rest * kXcds + kv % kXcds
+                                : dealt * per + rest * (heads - dealt) + (kv - dealt));
 }
 
 // The query rows [first_row, first_row + rows) of a unit (rows: token t, head h of the group, number t * group + h), what

@@ -22,6 +22,8 @@
 // Masked keys.  A weight of zero does not hide a value that is infinite or NaN from the product.  Rows hidden from all rows
 // of the workgroup are zeros in LDS; in the few tiles that some of its rows see and others do not (`edge`), values that
 // are not finite are taken out of the tile, remembered, and added for the rows that do see them (`add_odd`).
+#include <type_traits>
+
 #include "pages_attend.h"
 
 namespace scalekv {
@@ -41,6 +43,10 @@ struct Form {
   static constexpr int kKeyTiles = kBlock / 16;
   static constexpr int kRowBytes = D * kElem;            // in LDS
   static constexpr int kTileBytes = TN * kRowBytes;
+  // Keys in LDS as codes, widened where a wave takes them: only that wave does, and three workgroups fit a compute unit
+  // instead of two
+  static constexpr bool kKeyCodes = kBf16 && Q8 && WK > 1;
+  static constexpr int kKeyTileBytes = kKeyCodes ? TN * D : kTileBytes;
   static constexpr int kStages = WK == 1 && kBf16 ? 2 : 1;
   static constexpr int kSlabs = kRowBytes / 64;          // 16-byte operands of a query row that a lane holds
   static constexpr int kChans = D / 16;                  // 16-channel blocks of the output
@@ -48,36 +54,44 @@ struct Form {
   static constexpr int kSrcChunks = kSrcRow / 16;
   static constexpr int kVecs = TN * kSrcChunks / kThreads;  // 16-byte vectors of a tile of K, or of V, to a thread
   static constexpr int kRows = 16 * RT * WQ;             // query rows of a workgroup
+  static constexpr int kWavesPerSimd = kKeyCodes && RT == 1 ? 3 : 2;
   static constexpr int kJoinBytes = WK > 1 ? (WK - 1) * 64 * RT * (kChans * 16 + 8) : 0;
-  static constexpr int kLds = 2 * kStages * kTileBytes > kJoinBytes ? 2 * kStages * kTileBytes : kJoinBytes;
-  static_assert(4 * 16 * RT * D * 4 <= kLds, "the sums of all waves fit (add_odd)");
+  static constexpr int kSumBytes = 4 * 16 * RT * D * 4;  // of all waves, for add_odd()
+  static constexpr int kTilesBytes = kStages * (kKeyTileBytes + kTileBytes);
+  static constexpr int kLds = kTilesBytes > kJoinBytes ? kTilesBytes > kSumBytes ? kTilesBytes : kSumBytes
+                                                       : kJoinBytes > kSumBytes ? kJoinBytes : kSumBytes;
   __device__ static constexpr int k_flip(int r) { return kBf16 ? k_flip_bf16<D>(r) : r & 15; }
   __device__ static constexpr int v_flip(int r) { return kBf16 ? v_flip_bf16<D>(r) : r & 15; }
+  // rows of codes: the sixteen rows that lanes read eight codes of at a time differ in bits 0, 1, 3 and 4; with rows of 128
+  // bytes bit 0 already tells the halves of the banks apart, with rows of 64 bytes bits 0 and 1 the quarters
+  __device__ static constexpr int code_flip(int r) {
+    return D == 128 ? (r >> 1 & 1) | (r >> 3 & 1) << 1 | (r >> 4 & 1) << 2 : (r >> 3 & 1) | (r >> 4 & 1) << 1;
+  }
 };
 
 template <int TYPE, bool Q8, int D, int WQ, int RT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void pages_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<TYPE, Q8, D, WQ, RT>::kWavesPerSimd))) void pages_attend_kernel(AttendArgs a) {
   using F = Form<TYPE, Q8, D, WQ, RT>;
   constexpr bool BF16 = F::kBf16;
   constexpr int TN = F::TN, KT = F::kKeyTiles, NSL = F::kSlabs, NCB = F::kChans, NV = F::kVecs;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   __shared__ int any_odd;  // values that are not finite have been taken out of a tile
+  __shared__ uint8_t key_scale[F::kKeyCodes ? TN : 1];
   const PagesView& c = a.c;
 
   // ---- which query rows, which tiles
-  int unit, part_of;
-  unit_of(SCALEKV_WG_X, a.n_wg, a.n_split * a.n_row_group, unit, part_of);
-  const int split = part_of % a.n_split, row_group = part_of / a.n_split;
-  const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
+  const int wg = SCALEKV_WG_X;
+  const Slice slice = slice_of<TN>(a, wg);
+  if (slice.cuts == 0) return;
+  const int seq = slice.seq, kv = slice.kv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wq = wave % WQ, wk = wave / WQ;
-  const int first_row = row_group * F::kRows, wave_row = first_row + wq * (16 * RT);
-  if (first_row >= chunk_count(a.chunk, seq) * a.group) return;  // (rows of a split that are not written are not joined)
+  const int first_row = slice.row_group * F::kRows, wave_row = first_row + wq * (16 * RT);
   const Seen<TN> seen(a, seq, first_row, F::kRows);
   const int n_rows = seen.n_rows, pos0 = seen.pos0, sinks = seen.sinks;
-  const int per = (seen.n_tile + a.n_split - 1) / a.n_split;
-  const int t0 = min(split * per, seen.n_tile), t1 = min(t0 + per, seen.n_tile);
+  const int per = (seen.n_tile + slice.cuts - 1) / slice.cuts;
+  const int t0 = min(slice.cut * per, seen.n_tile), t1 = min(t0 + per, seen.n_tile);
 
   // ---- the query rows of this lane
   int q_end[RT], q_begin[RT], q_row[RT];
@@ -136,8 +150,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
   };
   auto store_rows = [&](int t, int stage) __attribute__((always_inline)) {
-    unsigned char* const k_lds = smem + stage * F::kTileBytes;
-    unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
+    unsigned char* const k_lds = smem + stage * F::kKeyTileBytes;
+    unsigned char* const v_lds = smem + F::kStages * F::kKeyTileBytes + stage * F::kTileBytes;
     const bool edge = seen.edge(t);
     constexpr int kOut = Q8 ? F::kElem : 1;  // vectors in LDS for one of the cache
 #pragma unroll
@@ -145,7 +159,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int row = ld_row + p * kRowsApart;
       u32x4 x[kOut], y[kOut];
       if constexpr (Q8) {
-        widen(kr[p], __uint_as_float((unsigned)ks[p] << 23), x);
+        if constexpr (F::kKeyCodes) {
+          *(u32x4*)(k_lds + row * D + 16 * (ld_chunk ^ F::code_flip(row))) = kr[p];
+          if (ld_chunk == 0) key_scale[row] = ks[p];
+        } else {
+          widen(kr[p], __uint_as_float((unsigned)ks[p] << 23), x);
+        }
         widen(vr[p], __uint_as_float((unsigned)vs[p] << 23), y);
       } else {
         x[0] = kr[p];
@@ -160,7 +179,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
       for (int w = 0; w < kOut; ++w) {
         const int chunk = ld_chunk * kOut + w;
-        *(u32x4*)(k_lds + row * F::kRowBytes + 16 * (chunk ^ F::k_flip(row))) = x[w];
+        if constexpr (!F::kKeyCodes) *(u32x4*)(k_lds + row * F::kRowBytes + 16 * (chunk ^ F::k_flip(row))) = x[w];
         *(u32x4*)(v_lds + row * F::kRowBytes + 16 * (chunk ^ F::v_flip(row))) = y[w];
       }
     }
@@ -180,14 +199,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   auto key_of = [&](int t, int v) { return BF16 ? 16 * (g & 1) + 8 * (g >> 1) + 4 * t + v : 4 * g + v; };
 
   auto work = [&](int t, int stage) __attribute__((always_inline)) {
-    const unsigned char* const k_lds = smem + stage * F::kTileBytes;
-    const unsigned char* const v_lds = smem + (F::kStages + stage) * F::kTileBytes;
+    const unsigned char* const k_lds = smem + stage * F::kKeyTileBytes;
+    const unsigned char* const v_lds = smem + F::kStages * F::kKeyTileBytes + stage * F::kTileBytes;
     const int key0 = seen.key0(t);
     const bool masked = key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > sinks);
 #pragma unroll
     for (int nb = 0; nb < F::kBlocks; ++nb) {
       const int block = wk * F::kBlocks + nb;
-      const unsigned char* const kb = k_lds + block * F::kBlock * F::kRowBytes;
+      const unsigned char* const kb = k_lds + block * F::kBlock * (F::kKeyCodes ? D : F::kRowBytes);
       const unsigned char* const vb = v_lds + block * F::kBlock * F::kRowBytes;
       f32x4 s[RT][KT];
 #pragma unroll
@@ -195,7 +214,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         const int row = BF16 ? 16 * (i >> 2 & 1) + 8 * (i >> 3) + (i & 3) + 4 * x : i;
         u32x4 kf[NSL];
 #pragma unroll
-        for (int sl = 0; sl < NSL; ++sl) kf[sl] = *(const u32x4*)(kb + row * F::kRowBytes + 16 * ((4 * sl + g) ^ F::k_flip(row)));
+        for (int sl = 0; sl < NSL; ++sl) {
+          if constexpr (F::kKeyCodes) {
+            const uint2 codes = *(const uint2*)(kb + row * D + 16 * ((2 * sl + g / 2) ^ F::code_flip(row)) + 8 * (g & 1));
+            const float scale = __uint_as_float((unsigned)key_scale[block * F::kBlock + row] << 23);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              kf[sl][e] = __builtin_bit_cast(unsigned, e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e < 2 ? codes.x : codes.y, scale, true)
+                                                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e < 2 ? codes.x : codes.y, scale, false));
+          } else {
+            kf[sl] = *(const u32x4*)(kb + row * F::kRowBytes + 16 * ((4 * sl + g) ^ F::k_flip(row)));
+          }
+        }
 #pragma unroll
         for (int b = 0; b < RT; ++b) s[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -370,8 +400,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   for (int b = 0; b < RT; ++b) {
     if (wave_row + 16 * b + i >= n_rows) continue;
     const int r = q_row[b], t = r / a.group, head = kv * a.group + (r - t * a.group);
-    if (a.n_split > 1) {
-      const long long row = ((long long)unit * a.chunk.max_new * a.group + r) * a.n_split + split;
+    if (slice.cuts > 1) {
+      const long long row = (long long)wg * a.part_rows + (r - first_row);
       if (g == 0) {
         a.stat[2 * row] = m_run[b] * a.scale_log2e;
         a.stat[2 * row + 1] = l_run[b];
@@ -398,57 +428,72 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
-// Adds up what the workgroups of a row have left: a wave to a row, D / 64 channels to a lane.
+// Adds up what the workgroups of a row group have left: a wave to a row, D / 64 channels to a lane.  A workgroup has
+// kJoinRows rows of one row group (most launches find little to do: keys are cut for long sequences alone).
+constexpr int kJoinRows = 32;
 template <int TYPE, int D>
-__global__ __launch_bounds__(kThreads) void pages_join_kernel(AttendArgs a, int n_rows_all) {
+__global__ __launch_bounds__(kThreads) void pages_join_kernel(AttendArgs a, int n_row_group, int join_groups) {
   constexpr int kPer = D / 64;
-  const int row = SCALEKV_WG_X * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= n_rows_all) return;
-  const int per_unit = a.chunk.max_new * a.group;
-  const int unit = row / per_unit, r = row - unit * per_unit, t = r / a.group;
-  const int seq = unit / a.c.n_kv_head, head = (unit - seq * a.c.n_kv_head) * a.group + (r - t * a.group);
-  if (t >= chunk_count(a.chunk, seq)) return;
-  const long long at = (long long)chunk_first(a.chunk, seq) + t;
-  if (at < 0 || at >= a.out.n_row) return;
-  const float* stat = a.stat + 2LL * row * a.n_split;
-  const float* part = a.part + (long long)row * a.n_split * D + kPer * lane;
-  float top = -INFINITY;
-  for (int x = 0; x < a.n_split; ++x) top = fmaxf(top, stat[2 * x]);
-  float sum = 0.f, o[kPer] = {};
-  for (int x = 0; x < a.n_split; ++x) {
-    const float l = stat[2 * x + 1];
-    if (l == 0.f) continue;  // no keys there, or none of any weight
-    const float f = __builtin_amdgcn_exp2f(stat[2 * x] - top);
-    sum += f * l;
+  const int wg = SCALEKV_WG_X, part_of = wg % join_groups, row_group = wg / join_groups % n_row_group;
+  const int unit = wg / join_groups / n_row_group, seq = unit / a.c.n_kv_head, kv = unit - seq * a.c.n_kv_head;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n_rows = __builtin_amdgcn_readfirstlane(chunk_count(a.chunk, seq)) * a.group;
+  const int first_row = row_group * a.rows;
+  if (first_row >= n_rows) return;
+  const int2 cut = a.cuts[seq];
+  const int cuts = __builtin_amdgcn_readfirstlane(cut.y);
+  if (cuts < 2) return;  // written already
+  const int n_group = (n_rows + a.rows - 1) / a.rows;
+  const int wg0 = workgroup_of(a, __builtin_amdgcn_readfirstlane(cut.x), cuts, n_group, kv, row_group, 0);
+  const long long rows_apart =
+      (long long)(workgroup_of(a, __builtin_amdgcn_readfirstlane(cut.x), cuts, n_group, kv, row_group, 1) - wg0) * a.part_rows;
+  const int end = min(min(first_row + a.rows, n_rows), first_row + (part_of + 1) * kJoinRows);
+  for (int r = first_row + part_of * kJoinRows + wave; r < end; r += kThreads / 64) {
+    const int t = r / a.group, head = kv * a.group + (r - t * a.group);
+    const long long at = (long long)chunk_first(a.chunk, seq) + t;
+    if (at < 0 || at >= a.out.n_row) continue;
+    const long long row0 = (long long)wg0 * a.part_rows + (r - first_row);
+    const float* const part = a.part + row0 * D + kPer * lane;
+    const float* const stat = a.stat + 2 * row0;
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int x = 0; x < cuts; ++x) top = fmaxf(top, stat[2 * x * rows_apart]);
+    float sum = 0.f, o[kPer] = {};
+#pragma unroll 4
+    for (int x = 0; x < cuts; ++x) {  // (a part without keys has sums of zero, at an offset far below all others)
+      const float f = __builtin_amdgcn_exp2f(stat[2 * x * rows_apart] - top);
+      sum += f * stat[2 * x * rows_apart + 1];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] += f * part[(long long)x * D + e];
-  }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
+      for (int e = 0; e < kPer; ++e) o[e] += f * part[x * rows_apart * D + e];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    if constexpr (TYPE == kTypeBf16) ((__bf16*)dst)[kPer * lane + e] = (__bf16)(o[e] * inv);
-    else ((float*)dst)[kPer * lane + e] = o[e] * inv;
+    for (int e = 0; e < kPer; ++e) {
+      const float y = sum == 0.f ? 0.f : o[e] * inv;
+      if constexpr (TYPE == kTypeBf16) ((__bf16*)dst)[kPer * lane + e] = (__bf16)y;
+      else ((float*)dst)[kPer * lane + e] = y;
+    }
   }
 }
 
 template <int TYPE, bool Q8, int D, int WQ, int RT>
-hipError_t launch_form(const AttendArgs& a, hipStream_t stream) {
+hipError_t launch_form(const AttendArgs& a, int n_wg, hipStream_t stream) {
   using F = Form<TYPE, Q8, D, WQ, RT>;
   static std::atomic<uint64_t> done{0};
   const hipError_t e = allow_dynamic_lds((const void*)pages_attend_kernel<TYPE, Q8, D, WQ, RT>, F::kLds, done);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((pages_attend_kernel<TYPE, Q8, D, WQ, RT>), dim3(a.n_wg), dim3(kThreads), F::kLds, stream, a);
+  hipLaunchKernelGGL((pages_attend_kernel<TYPE, Q8, D, WQ, RT>), dim3(n_wg), dim3(kThreads), F::kLds, stream, a);
   return hipGetLastError();
 }
 
 template <int TYPE, bool Q8, int D>
 hipError_t launch_plan(const PagesPlan& plan, const AttendArgs& a, hipStream_t stream) {
   if constexpr (TYPE == kTypeBf16) {
-    if (plan.row_waves == 4) return launch_pages_chunk(D, Q8, plan.row_tiles, a, stream);
-    return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 1, 2>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);
+    if (plan.row_waves == 4) return launch_pages_chunk(D, Q8, plan.row_tiles, a, plan.n_wg, stream);
+    return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 1, 2>(a, plan.n_wg, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, plan.n_wg, stream);
   } else {
-    return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4, 1>(a, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, stream);
+    return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4, 1>(a, plan.n_wg, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, plan.n_wg, stream);
   }
 }
 
@@ -458,14 +503,6 @@ PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& p
   constexpr int kComputeUnits = 256;
   const int rows = max_new * (n_head / pages.n_kv_head);
   PagesPlan p{};
-  if (dtype == kTypeF32) {
-    p.row_waves = rows <= 16 ? 1 : 4;
-    p.row_tiles = 1;
-  } else {
-    p.row_waves = rows <= 32 ? 1 : 4;
-    p.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
-  }
-  p.n_row_group = (rows + p.rows() - 1) / p.rows();
   // keys that a row group can see at most
   const long long cap = (long long)pages.width << pages.page_shift;
   long long keys = cap;
@@ -473,11 +510,33 @@ PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& p
     const long long seen = (long long)mask.n_sink + mask.window + max_new;
     keys = seen < cap ? seen : cap;
   }
-  const long long groups = (long long)n_seq * pages.n_kv_head * p.n_row_group;
-  long long split = 4 * kComputeUnits / groups;            // four workgroups to a compute unit
-  const long long most = keys / (p.row_waves == 1 ? 256 : 512);  // not worth a join below that
-  split = split < most ? split : most;
-  p.n_split = (int)(split < 1 ? 1 : split > 64 ? 64 : split);
+  // The fewest rows that hold a unit's, up to 128 (fp32: 16 or 64), and fewer where that leaves compute units without work
+  // that the keys, cut into pieces of min_tiles tiles, do not give them either.
+  struct Rows {
+    int waves, tiles;
+  };
+  static constexpr Rows kBf16[] = {{1, 1}, {1, 2}, {4, 1}, {4, 2}}, kF32[] = {{1, 1}, {4, 1}};
+  const Rows* const forms = dtype == kTypeF32 ? kF32 : kBf16;
+  int form = dtype == kTypeF32 ? 1 : 3;
+  const long long units = (long long)n_seq * pages.n_kv_head, all_rows = (long long)n_seq * n_head * max_new;
+  long long groups = 0, tiles = 0;
+  for (bool fits = true; fits; --form) {
+    p.row_waves = forms[form].waves;
+    p.row_tiles = forms[form].tiles;
+    const int tile = dtype == kTypeF32 || p.row_waves == 4 ? 64 : 128;
+    tiles = (keys + tile - 1) / tile + (keys < cap ? 2 : 0);
+    p.min_tiles = p.row_waves == 4 ? 16 : all_rows <= 512 ? 1 : dtype == kTypeF32 ? 16 : 8;
+    groups = units * ((rows + p.rows() - 1) / p.rows());
+    const long long parts = groups * (tiles > p.min_tiles ? tiles / p.min_tiles : 1);
+    fits = form > 0 && (rows <= p.rows() / 2 || parts < kComputeUnits);
+  }
+  p.target = (p.row_waves == 4 ? 4 : 2) * kComputeUnits;
+  // (a window bounds what a sequence costs: enough row groups are then enough)
+  if (tiles <= p.min_tiles || groups >= 4 * p.target || (keys < cap && groups >= p.target)) p.target = 0;
+  // every sequence's tiles over `most` are rounded up, once to a group
+  const long long cut = groups + p.target, parts = groups * ((tiles + p.min_tiles - 1) / p.min_tiles);
+  const long long n_wg = p.target == 0 ? groups : cut < parts ? cut : parts;
+  p.n_wg = n_wg <= 0x7fffffff ? (int)n_wg : -1;
   return p;
 }
 
@@ -492,14 +551,16 @@ hipError_t launch_pages_attend(int dtype, int d, int n_seq, int n_head, const Pa
   a.mask = mask;
   a.n_seq = n_seq;
   a.group = n_head / pages.n_kv_head;
-  a.n_row_group = plan.n_row_group;
-  a.n_split = plan.n_split;
-  a.n_wg = n_seq * pages.n_kv_head * plan.n_row_group * plan.n_split;
+  a.rows = plan.rows();
+  a.target = plan.target;
+  a.min_tiles = plan.min_tiles;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
   a.no_max = no_maximum(a.scale_log2e);
-  const int n_rows = n_seq * n_head * chunk.max_new;
+  const size_t part_rows = pages_partial_rows(a.group, chunk.max_new, plan);
+  a.part_rows = (int)(part_rows / plan.n_wg);
   a.part = (float*)ws;
-  a.stat = a.part + (size_t)n_rows * plan.n_split * d;
+  a.stat = a.part + part_rows * d;
+  a.cuts = (int2*)(a.stat + part_rows * 2);
   const bool q8 = pages.type == kTypeE4m3;
   hipError_t e;
   if (dtype == kTypeBf16) {
@@ -509,15 +570,19 @@ hipError_t launch_pages_attend(int dtype, int d, int n_seq, int n_head, const Pa
     if (d == 128) e = q8 ? launch_plan<kTypeF32, true, 128>(plan, a, stream) : launch_plan<kTypeF32, false, 128>(plan, a, stream);
     else e = q8 ? launch_plan<kTypeF32, true, 64>(plan, a, stream) : launch_plan<kTypeF32, false, 64>(plan, a, stream);
   }
-  if (e != hipSuccess || plan.n_split == 1) return e;
-  const dim3 grid((n_rows + 3) / 4);
-  if (dtype == kTypeBf16) {
-    if (d == 128) hipLaunchKernelGGL((pages_join_kernel<kTypeBf16, 128>), grid, dim3(kThreads), 0, stream, a, n_rows);
-    else hipLaunchKernelGGL((pages_join_kernel<kTypeBf16, 64>), grid, dim3(kThreads), 0, stream, a, n_rows);
-  } else {
-    if (d == 128) hipLaunchKernelGGL((pages_join_kernel<kTypeF32, 128>), grid, dim3(kThreads), 0, stream, a, n_rows);
-    else hipLaunchKernelGGL((pages_join_kernel<kTypeF32, 64>), grid, dim3(kThreads), 0, stream, a, n_rows);
-  }
+  if (e != hipSuccess || plan.target == 0) return e;
+  const int unit_rows = chunk.max_new * a.group, n_row_group = (unit_rows + a.rows - 1) / a.rows;
+  const int join_groups = ((unit_rows < a.rows ? unit_rows : a.rows) + kJoinRows - 1) / kJoinRows;
+  const dim3 grid((unsigned)(n_seq * pages.n_kv_head * n_row_group * join_groups));
+  auto join = [&](auto type, auto dim) {
+    hipLaunchKernelGGL((pages_join_kernel<type(), dim()>), grid, dim3(kThreads), 0, stream, a, n_row_group, join_groups);
+  };
+  auto of_dim = [&](auto type) {
+    if (d == 128) join(type, std::integral_constant<int, 128>{});
+    else join(type, std::integral_constant<int, 64>{});
+  };
+  if (dtype == kTypeBf16) of_dim(std::integral_constant<int, kTypeBf16>{});
+  else of_dim(std::integral_constant<int, kTypeF32>{});
   return hipGetLastError();
 }
 

@@ -60,19 +60,16 @@ void pages_chunk_kernel(AttendArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const PagesView& c = a.c;
 
-  int unit, part_of;
-  unit_of(SCALEKV_WG_X, a.n_wg, a.n_split * a.n_row_group, unit, part_of);
-  // under a causal mask later rows see more: they come first, so that the short ones fill up the end
-  const int split = part_of % a.n_split, nth = part_of / a.n_split;
-  const int row_group = a.mask.causal ? a.n_row_group - 1 - nth : nth;
-  const int seq = unit / c.n_kv_head, kv = unit - seq * c.n_kv_head;
+  const int wg = SCALEKV_WG_X;
+  const Slice slice = slice_of<TN>(a, wg);
+  if (slice.cuts == 0) return;
+  const int seq = slice.seq, kv = slice.kv;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int first_row = row_group * G::kRows, wave_row = first_row + wave * (16 * RT);
-  if (first_row >= chunk_count(a.chunk, seq) * a.group) return;
+  const int first_row = slice.row_group * G::kRows, wave_row = first_row + wave * (16 * RT);
   const Seen<TN> seen(a, seq, first_row, G::kRows);
-  const int per = (seen.n_tile + a.n_split - 1) / a.n_split;
-  const int t0 = min(split * per, seen.n_tile), n_tile = min(t0 + per, seen.n_tile) - t0;
+  const int per = (seen.n_tile + slice.cuts - 1) / slice.cuts;
+  const int t0 = min(slice.cut * per, seen.n_tile), n_tile = min(t0 + per, seen.n_tile) - t0;
   // all rows of the wave see [w_begin, w_end) and the sinks below w_end
   const int w_end = seen.end_of(seen.pos0 + min(wave_row, seen.n_rows - 1) / a.group);
   const int w_begin = seen.begin_of(seen.pos0 + min(wave_row + 16 * RT - 1, seen.n_rows - 1) / a.group);
@@ -529,18 +526,33 @@ void pages_chunk_kernel(AttendArgs a) {
   // ---- write
 #pragma unroll
   for (int b = 0; b < RT; ++b) l_run[b] = xor32_sum(xor16_sum(l_run[b]));
-  if (a.n_split > 1) {
+  if (slice.cuts > 1) {
+    // whole rows here too, 16 of them at a time
+    constexpr int kSumStride = D * 4 + 16, kLanes = D / 4;
+    static_assert(16 * kSumStride <= 16 * RT * D * 4 || RT == 1, "16 rows of sums fit in a wave's part");
+    unsigned char* const sums = smem + wave * (16 * kSumStride);
+    static_assert(kWaves * 16 * kSumStride <= G::kLds, "and those of all waves in the tiles' place");
 #pragma unroll
     for (int b = 0; b < RT; ++b) {
-      const int r = wave_row + 16 * b + i;
-      if (r >= seen.n_rows) continue;
-      const long long row = ((long long)unit * a.chunk.max_new * a.group + r) * a.n_split + split;
-      if (g == 0) {
-        a.stat[2 * row] = -neg[b];
-        a.stat[2 * row + 1] = l_run[b];
+      const long long row = (long long)wg * a.part_rows + (wave_row - first_row) + 16 * b;
+      if (g == 0 && wave_row + 16 * b + i < seen.n_rows) {
+        a.stat[2 * (row + i)] = -neg[b];
+        a.stat[2 * (row + i) + 1] = l_run[b];
       }
 #pragma unroll
-      for (int x = 0; x < NCB; ++x) *(f32x4*)(a.part + row * D + 16 * x + 4 * g) = o[b][x];
+      for (int x = 0; x < NCB; ++x) *(f32x4*)(sums + i * kSumStride + 64 * x + 16 * g) = o[b][x];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int p = 0; p < 16 * kLanes / 64; ++p) {
+        const int r = (64 / kLanes) * p + lane / kLanes;
+        const f32x4 val = *(const f32x4*)(sums + r * kSumStride + 16 * (lane % kLanes));
+        if (wave_row + 16 * b + r < seen.n_rows) *(f32x4*)(a.part + (row + r) * D + 4 * (lane % kLanes)) = val;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
     return;
   }
@@ -575,20 +587,20 @@ void pages_chunk_kernel(AttendArgs a) {
 }
 
 template <int D, bool Q8, int RT>
-hipError_t launch_form(const AttendArgs& a, hipStream_t stream) {
+hipError_t launch_form(const AttendArgs& a, int n_wg, hipStream_t stream) {
   using G = Chunk<D, Q8, RT>;
   static std::atomic<uint64_t> done{0};
   const hipError_t e = allow_dynamic_lds((const void*)pages_chunk_kernel<D, Q8, RT>, G::kLds, done);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((pages_chunk_kernel<D, Q8, RT>), dim3(a.n_wg), dim3(64 * kWaves), G::kLds, stream, a);
+  hipLaunchKernelGGL((pages_chunk_kernel<D, Q8, RT>), dim3(n_wg), dim3(64 * kWaves), G::kLds, stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, hipStream_t stream) {
+hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, int n_wg, hipStream_t stream) {
   auto tiles = [&](auto dim, auto quantised) {
-    return row_tiles == 2 ? launch_form<dim(), quantised(), 2>(a, stream) : launch_form<dim(), quantised(), 1>(a, stream);
+    return row_tiles == 2 ? launch_form<dim(), quantised(), 2>(a, n_wg, stream) : launch_form<dim(), quantised(), 1>(a, n_wg, stream);
   };
   auto cache = [&](auto dim) { return q8 ? tiles(dim, std::true_type{}) : tiles(dim, std::false_type{}); };
   return d == 64 ? cache(std::integral_constant<int, 64>{}) : cache(std::integral_constant<int, 128>{});

@@ -58,6 +58,13 @@ def _check_attend(seed, seqs, heads, kv_heads, d, dtype, cache_dtype, page, most
     return got
 
 
+def _attend(shape, pages, q, out, new, **kw):
+    """pages_attend with a workspace of the size that it asks for."""
+    mask = {x: kw[x] for x in ("causal", "window", "n_sink") if x in kw}
+    ws = torch.full((skv.pages_workspace_bytes(shape, pages, new, **mask),), 255, dtype=torch.uint8, device=DEV)
+    skv.pages_attend(shape, pages, q, out, ws, max_new=new, **kw)
+
+
 TYPES = [(BF16, BF16), (BF16, E4M3), (F32, F32), (F32, E4M3)]
 
 
@@ -275,7 +282,7 @@ def test_tokens_that_see_nothing_get_zeros(dtype, cache_dtype):
     pages = cache.on(DEV)
     q = torch.randn(3, heads, new, d, generator=torch.Generator().manual_seed(2)).to(dtype)
     out = torch.full((3, heads, new, d), 7.0, dtype=dtype, device=DEV)
-    skv.pages_attend(shape, pages, q.to(DEV), out, None, causal=True)
+    _attend(shape, pages, q.to(DEV), out, new, causal=True)
     torch.cuda.synchronize()
     assert torch.all(out[0, :, :5] == 0) and torch.all(out[1] == 0)
     want, tol = P.attend(cache, 0, q[0, :, 5:], True, 0, 0, d ** -0.5)
@@ -290,7 +297,7 @@ def test_all_scores_minus_infinity_give_zeros_not_nan():
     cache.pool["k"].fill_(-math.inf)
     q = torch.ones(1, 1, 3, d)
     out = torch.full((1, 1, 3, d), 7.0, device=DEV)
-    skv.pages_attend(skv.Shape(1, 1, d, dtype), cache.on(DEV), q.to(DEV), out, None, causal=True)
+    _attend(skv.Shape(1, 1, d, dtype), cache.on(DEV), q.to(DEV), out, 3, causal=True)
     assert torch.all(out == 0)
 
 
@@ -307,7 +314,7 @@ def test_values_out_of_range_lead_nowhere(dtype, cache_dtype):
     q = torch.randn(seqs, heads, 5, d, generator=torch.Generator().manual_seed(2)).to(dtype)
     out = torch.full((seqs, heads, 5, d), 7.0, dtype=dtype, device=DEV)
     count = torch.tensor([5, -3, 100], dtype=torch.int32, device=DEV)  # 5, 0 and 5 tokens
-    skv.pages_attend(shape, pages, q.to(DEV), out, None, causal=True, count=count, max_new=5)
+    _attend(shape, pages, q.to(DEV), out, 5, causal=True, count=count)
     torch.cuda.synchronize()
     for s in (0, 2):
         want, tol = P.attend(cache, s, q[s], True, 0, 0, d ** -0.5)
@@ -322,8 +329,8 @@ def test_values_out_of_range_lead_nowhere(dtype, cache_dtype):
     skv.pages_write(shape, pages, x[0].transpose(0, 1), x[0].transpose(0, 1), first=first,
                     count=torch.tensor([1, 2, 2], dtype=torch.int32, device=DEV), max_new=2)
     o = torch.full((2, heads, d), 7.0, dtype=dtype, device=DEV)
-    skv.pages_attend(shape, pages, x[0].transpose(0, 1), o, None, first=first,
-                     count=torch.tensor([1, 2, 2], dtype=torch.int32, device=DEV), max_new=2)
+    _attend(shape, pages, x[0].transpose(0, 1), o, 2, first=first,
+            count=torch.tensor([1, 2, 2], dtype=torch.int32, device=DEV))
     torch.cuda.synchronize()
     assert torch.equal(before[0], pages.k.view(torch.uint8)) and torch.equal(before[1], pages.v.view(torch.uint8))
     assert torch.all(o == 7.0)
@@ -343,7 +350,7 @@ def test_strides_and_orders(dtype, cache_dtype):
     on = fused.to(DEV)
     q, k, v = (on[:, :, a:b].transpose(1, 2) for a, b in ((0, heads), (heads, heads + kv_heads), (heads + kv_heads, None)))
     skv.pages_write(shape, pages, k, v)
-    skv.pages_attend(shape, pages, q, q, None, causal=True)
+    _attend(shape, pages, q, q, new, causal=True)
     torch.cuda.synchronize()
     for name, t in (("k", view(0)), ("v", view(1))):
         cache.pool[name] = t.cpu()

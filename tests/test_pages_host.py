@@ -184,9 +184,11 @@ def test_keys_and_values_that_share_bytes_are_refused(L):
 
 
 def test_the_workspace_covers_every_size_and_is_not_asked_for_where_rows_abound(L):
+    # sums of every workgroup that there may be: no more than keys can be cut for, and than there are tiles of 128 keys
     for n_seq, heads, kv, width, new in ((1, 8, 1, 4096, 1), (2, 32, 8, 4096, 1), (1, 1, 1, 1, 1), (64, 32, 8, 125, 1)):
         st, need = _need(L, _shape(n_seq=n_seq, n_head=heads), _pages(n_kv_head=kv, table_width=width), new)
-        assert st == OK and need % 4 == 0 and need <= 64 * n_seq * heads * new * 130 * 4
+        units, parts = n_seq * kv, -(-width * 32 // 128)
+        assert st == OK and need % 4 == 0 and need <= min(512 + units, units * parts) * heads // kv * 130 * 4 + 8 * n_seq
     assert _need(L, _shape(n_seq=16, n_head=16), _pages(n_kv_head=16, table_width=200), 4096) == (OK, 0)
 
 
