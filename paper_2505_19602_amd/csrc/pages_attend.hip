@@ -187,12 +187,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
 
   // ---- state of the rows
   f32x4 o[RT][NCB];
-  float m_run[RT], l_run[RT];  // largest logit (the same in the four lanes of a row), this lane's share of the sum
+  // Less the offset of a row, its largest logit in log2 units (the same in the four lanes of a row), and this lane's share of
+  // the sum.  The offset is kept as it has been rounded: factors between offsets are then exactly those between the weights
+  // (formed from the logits anew they are off by the rounding of the product, 2^-24 of its magnitude).
+  float neg[RT], l_run[RT];
 #pragma unroll
   for (int b = 0; b < RT; ++b) {
 #pragma unroll
     for (int x = 0; x < NCB; ++x) o[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m_run[b] = a.no_max;
+    neg[b] = -(a.no_max * a.scale_log2e);
     l_run[b] = 0.f;
   }
   // key of register v of key tile t, in a block
@@ -203,7 +206,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     const unsigned char* const v_lds = smem + F::kStages * F::kKeyTileBytes + stage * F::kTileBytes;
     const int key0 = seen.key0(t);
     const bool masked = key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > sinks);
-#pragma unroll
+#pragma unroll 1  // (blocks side by side spill registers)
     for (int nb = 0; nb < F::kBlocks; ++nb) {
       const int block = wk * F::kBlocks + nb;
       const unsigned char* const kb = k_lds + block * F::kBlock * (F::kKeyCodes ? D : F::kRowBytes);
@@ -226,22 +229,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
             kf[sl] = *(const u32x4*)(kb + row * F::kRowBytes + 16 * ((4 * sl + g) ^ F::k_flip(row)));
           }
         }
+        if constexpr (BF16) {
 #pragma unroll
-        for (int b = 0; b < RT; ++b) s[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int b = 0; b < RT; ++b) s[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int sl = 0; sl < NSL; ++sl)
+          for (int sl = 0; sl < NSL; ++sl)
 #pragma unroll
-          for (int b = 0; b < RT; ++b) {
-            if constexpr (BF16) {
+            for (int b = 0; b < RT; ++b)
               s[b][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sl]),
                                                                 __builtin_bit_cast(bf16x8, qf[b][sl]), s[b][x], 0, 0, 0);
-            } else {
+        } else {
+          // four sums of every fourth channel: shorter chains, of instructions and of roundings
+#pragma unroll
+          for (int b = 0; b < RT; ++b) {
+            f32x4 sum[4];
+#pragma unroll
+            for (int sl = 0; sl < NSL; ++sl)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                s[b][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sl][e]), __uint_as_float(qf[b][sl][e]),
-                                                               s[b][x], 0, 0, 0);
-            }
+                sum[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sl][e]), __uint_as_float(qf[b][sl][e]),
+                                                              sl ? sum[e] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            s[b][x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
           }
+        }
       }
       if (masked) {
 #pragma unroll
@@ -254,7 +264,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
               if (pos >= q_end[b] || (pos < q_begin[b] && pos >= sinks)) s[b][x][v] = -INFINITY;
           }
       }
-      // running maximum, moved only where it has grown by more than kRescaleThreshold
+      // Running maximum, moved only where it has grown by more than kRescaleThreshold; in fp32 wherever it has grown, so that
+      // the exponents of the weights that count are small, and with them the rounding of an exponent.
       float mx[RT];
       bool grow = false;
 #pragma unroll
@@ -263,14 +274,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
 #pragma unroll
         for (int y = 1; y < 4 * KT; ++y) m = fmaxf(m, s[b][y / 4][y % 4]);
         mx[b] = xor32_max(xor16_max(m));
-        grow |= (mx[b] - m_run[b]) * a.scale_log2e > kRescaleThreshold;
+        grow |= fmaf(mx[b], a.scale_log2e, neg[b]) > (BF16 ? kRescaleThreshold : 0.f);
       }
       if (__builtin_amdgcn_ballot_w64(grow) != 0) {
 #pragma unroll
         for (int b = 0; b < RT; ++b) {
-          const float m_new = fmaxf(m_run[b], mx[b]);
-          const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
-          m_run[b] = m_new;
+          const float now = fminf(neg[b], -(mx[b] * a.scale_log2e));
+          const float alpha = __builtin_amdgcn_exp2f(now - neg[b]);
+          neg[b] = now;
           l_run[b] *= alpha;
 #pragma unroll
           for (int x = 0; x < NCB; ++x) o[b][x] *= alpha;
@@ -280,9 +291,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       u32x4 p[RT];
 #pragma unroll
       for (int b = 0; b < RT; ++b) {
-        const float neg = -(m_run[b] * a.scale_log2e);
 #pragma unroll
-        for (int y = 0; y < 4 * KT; ++y) w[b][y] = __builtin_amdgcn_exp2f(fmaf(s[b][y / 4][y % 4], a.scale_log2e, neg));
+        for (int y = 0; y < 4 * KT; ++y) w[b][y] = __builtin_amdgcn_exp2f(fmaf(s[b][y / 4][y % 4], a.scale_log2e, neg[b]));
         if constexpr (BF16) {
           // (weights are rounded to bf16 for the matrix cores; the sum adds the rounded ones)
 #pragma unroll
@@ -346,13 +356,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       __syncthreads();
     }
     if (any_odd && wave_row < n_rows) {
-      float less[RT];
-#pragma unroll
-      for (int b = 0; b < RT; ++b) less[b] = -(m_run[b] * a.scale_log2e);
       float* const sums = (float*)smem + wave * (16 * RT * D);
       sums_to_lds<D, RT>(o, sums);
       constexpr int kMine = F::kBlocks * F::kBlock;
-      add_odd<TYPE, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t1, wk * kMine, (wk + 1) * kMine, less, sums);
+      add_odd<TYPE, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t1, wk * kMine, (wk + 1) * kMine, neg, sums);
       sums_from_lds<D, RT>(o, sums);
     }
   }
@@ -369,7 +376,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       for (int b = 0; b < RT; ++b) {
 #pragma unroll
         for (int ch = 0; ch < NCB; ++ch) part[(((wk - 1) * RT + b) * NCB + ch) * 64 + lane] = o[b][ch];
-        stat[(((wk - 1) * RT + b) * 2) * 64 + lane] = m_run[b];
+        stat[(((wk - 1) * RT + b) * 2) * 64 + lane] = neg[b];
         stat[(((wk - 1) * RT + b) * 2 + 1) * 64 + lane] = l_run[b];
       }
     }
@@ -377,21 +384,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if (wk > 0) return;
 #pragma unroll
     for (int b = 0; b < RT; ++b) {
-      float top = m_run[b];
+      float now = neg[b];
 #pragma unroll
-      for (int x = 0; x < F::WK - 1; ++x) top = fmaxf(top, stat[((x * RT + b) * 2) * 64 + lane]);
-      const float own = __builtin_amdgcn_exp2f((m_run[b] - top) * a.scale_log2e);
+      for (int x = 0; x < F::WK - 1; ++x) now = fminf(now, stat[((x * RT + b) * 2) * 64 + lane]);
+      const float own = __builtin_amdgcn_exp2f(now - neg[b]);
       l_run[b] *= own;
 #pragma unroll
       for (int ch = 0; ch < NCB; ++ch) o[b][ch] *= own;
 #pragma unroll
       for (int x = 0; x < F::WK - 1; ++x) {
-        const float f = __builtin_amdgcn_exp2f((stat[((x * RT + b) * 2) * 64 + lane] - top) * a.scale_log2e);
+        const float f = __builtin_amdgcn_exp2f(now - stat[((x * RT + b) * 2) * 64 + lane]);
         l_run[b] += f * stat[((x * RT + b) * 2 + 1) * 64 + lane];
 #pragma unroll
         for (int ch = 0; ch < NCB; ++ch) o[b][ch] += f * part[((x * RT + b) * NCB + ch) * 64 + lane];
       }
-      m_run[b] = top;
+      neg[b] = now;
     }
   }
 
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if (slice.cuts > 1) {
       const long long row = (long long)wg * a.part_rows + (r - first_row);
       if (g == 0) {
-        a.stat[2 * row] = m_run[b] * a.scale_log2e;
+        a.stat[2 * row] = -neg[b];
         a.stat[2 * row + 1] = l_run[b];
       }
 #pragma unroll
