@@ -37,7 +37,9 @@ struct Chunk {
   static constexpr int kRows = 16 * RT * kWaves;
   static constexpr int kWavesPerSimd = D == 128 ? 2 : 3;
   static constexpr int kLds = 4 * kTileBytes + (Q8 ? 2 * kWaves * 16 * D : 0);  // two stages of K, two of V; codes
-  static_assert(kWaves * 16 * RT * D * 4 <= kLds, "the sums of all waves fit (add_odd)");
+  // a wave's part of the LDS behind the tile loop: its sums (add_odd), 16 rows of them with padding, or its output
+  static constexpr int kMine = 16 * RT * D * 4 > 16 * (D * 4 + 16) ? 16 * RT * D * 4 : 16 * (D * 4 + 16);
+  static_assert(kWaves * kMine <= kLds, "fits in the tiles' place");
 };
 
 // 16 bytes a lane from base + voff straight into LDS, at lds_addr + 16 lane (attend_pipe.hip has the reasons for assembly);
@@ -515,7 +517,7 @@ void pages_chunk_kernel(AttendArgs a) {
   }
   if (wave_row >= seen.n_rows) return;
   // (each wave has a part of the LDS to itself from here on, for add_odd() and then for its output)
-  unsigned char* const mine = smem + wave * (16 * RT * D * 4);
+  unsigned char* const mine = smem + wave * G::kMine;
   if (any_odd) {
     float* const sums = (float*)mine;
     sums_to_lds<D, RT>(o, sums);
@@ -529,9 +531,7 @@ void pages_chunk_kernel(AttendArgs a) {
   if (slice.cuts > 1) {
     // whole rows here too, 16 of them at a time
     constexpr int kSumStride = D * 4 + 16, kLanes = D / 4;
-    static_assert(16 * kSumStride <= 16 * RT * D * 4 || RT == 1, "16 rows of sums fit in a wave's part");
-    unsigned char* const sums = smem + wave * (16 * kSumStride);
-    static_assert(kWaves * 16 * kSumStride <= G::kLds, "and those of all waves in the tiles' place");
+    unsigned char* const sums = mine;
 #pragma unroll
     for (int b = 0; b < RT; ++b) {
       const long long row = (long long)wg * a.part_rows + (wave_row - first_row) + 16 * b;

@@ -246,7 +246,7 @@ def test_attend_scores_that_rise_and_fall(dtype, cache_dtype, new):
 @pytest.mark.parametrize("window", [0, 5, 40])
 def test_what_a_token_does_not_see_does_not_reach_it(dtype, d, value, window):
     # values and keys that are not finite, in rows that some tokens of a tile see and others do not
-    for new, rows, group in ((40, 40, 1), (130, 200, 1), (6, 70, 4), (1, 90, 1), (3, 700, 8)):
+    for new, rows, group in ((40, 40, 1), (130, 200, 1), (6, 70, 4), (1, 90, 1), (3, 700, 8), (130, 3500, 1), (70, 2500, 1)):
         bad = {0, 3, rows - new + new // 2, rows - 1, rows - 2, max(0, rows - 45)}
 
         def change(cache):
