@@ -351,7 +351,7 @@ typedef struct {
 /* Rows of new tokens, in any order of sequence, head and token: element 0 of row i of head h of sequence s is
  * ptr + s * seq_stride + h * head_stride + i * row_stride (elements, >= 0, multiples of 16 bytes; a row is contiguous). */
 typedef struct {
-  void* ptr; /* device, 16-byte aligned */
+  void* ptr; /* device, 16-byte aligned; may be NULL where packed tensors have no rows: nothing is done then */
   int64_t seq_stride, head_stride, row_stride;
   int32_t n_row; /* rows of a sequence; of all sequences where they are packed one behind the other (seq_stride 0) */
 } scalekv_rows;
@@ -411,7 +411,8 @@ scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pa
  * [n_seq]; count and first [n_seq] (NULL as in `chunk`, whose own pointers are not read; chunk NULL: nothing is new);
  * n_row: of the tensors that hold the new tokens.  INVALID_ARG, and a message that names the entry, for: a
  * length outside [0, table_width * page_rows]; a page in use outside [0, n_page); a count outside [0, min(max_new, len)];
- * token rows outside [0, n_row); a page that receives new tokens and is used by another sequence or twice by one. */
+ * token rows outside [0, n_row); a page that receives new tokens and is used by another sequence or twice by one (each
+ * page that receives tokens is looked for in all tables). */
 scalekv_status scalekv_pages_check(const scalekv_shape* shape, const scalekv_pages* pages,
                                    const int32_t* table, const int32_t* len,
                                    const scalekv_chunk* chunk, const int32_t* first,

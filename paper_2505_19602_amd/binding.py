@@ -608,7 +608,8 @@ class Pages:
     k, v [n_page, n_kv_head, page_rows, d] (views with larger page and head strides are fine; the same strides for both)
     of the shape's dtype or torch.float8_e4m3fn, which needs k_scale, v_scale [n_page, n_kv_head, page_rows] uint8 beside
     it; table [S, width] int32: the pages of each sequence; lens [S] int32: its rows, new tokens among them.  Table and
-    lengths are read when a call's kernels run: they may be changed between calls, and between replays of a captured call.
+    lengths are read when a call's kernels run: their contents may be changed between calls, and between replays of a
+    captured call.  The tensors themselves are those of the object for good.
     """
 
     __slots__ = ("k", "v", "table", "lens", "k_scale", "v_scale", "c", "_native")
@@ -639,11 +640,16 @@ class Pages:
             raise ScaleKVError(1, f"table must be [S, width], got {tuple(table.shape)}")
         _int_tensor(table, table.shape, "table")
         _int_tensor(lens, table.shape[:1], "lens")
-        self.k, self.v, self.table, self.lens, self.k_scale, self.v_scale = k, v, table, lens, k_scale, v_scale
-        self.c = _CPages(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(),
+        put = lambda name, value: object.__setattr__(self, name, value)
+        for name, t in (("k", k), ("v", v), ("table", table), ("lens", lens), ("k_scale", k_scale), ("v_scale", v_scale)):
+            put(name, t)
+        put("c", _CPages(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(),
                          0 if v_scale is None else v_scale.data_ptr(), *strides[0], *scale_strides[0], n_page, heads, rows,
-                         _CACHE_DTYPES[k.dtype], table.data_ptr(), table.shape[1], lens.data_ptr())
-        self._native = (ctypes.addressof(self.c), table.shape[0], d, k.device.index)   # for csrc/marshal.cpp
+                         _CACHE_DTYPES[k.dtype], table.data_ptr(), table.shape[1], lens.data_ptr()))
+        put("_native", (ctypes.addressof(self.c), table.shape[0], d, k.device.index))   # for csrc/marshal.cpp
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: the pointers of a Pages object are taken when it is made; make another one")
 
     @staticmethod
     def _strides(t, unit, sizes, name):

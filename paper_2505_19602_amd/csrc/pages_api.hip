@@ -81,6 +81,7 @@ scalekv_status check_chunk(const scalekv_shape* s, const scalekv_chunk* chunk) {
 
 scalekv_status check_token_rows(const scalekv_shape* s, const scalekv_rows* r, const scalekv_chunk* chunk, const char* name) {
   if (!r) return fail(SCALEKV_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!r->ptr && r->n_row == 0 && chunk->first) return SCALEKV_OK;  // packed, and no sequence has new tokens
   if (!r->ptr) return fail(SCALEKV_ERR_INVALID_ARG, "%s.ptr is NULL", name);
   if (!aligned16(r->ptr)) return fail(SCALEKV_ERR_INVALID_ARG, "%s.ptr is not 16-byte aligned", name);
   const int per = 16 / elem_bytes(s);
@@ -214,6 +215,7 @@ scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pag
         if (meet(pool_span(shape, pages, p), scale_span(pages, q)))
           return fail(SCALEKV_ERR_INVALID_ARG, "the scales overlap the pool");
   }
+  if (k_new->n_row == 0 && v_new->n_row == 0) return SCALEKV_OK;
   SCALEKV_HIP(launch_pages_write(shape->dtype, shape->head_dim, shape->n_seq, pages_view(shape, pages),
                                  rows_view(shape, k_new), rows_view(shape, v_new),
                                  ChunkView{chunk->max_new, chunk->first, chunk->count}, static_cast<hipStream_t>(stream)),
@@ -268,6 +270,7 @@ scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pa
   SCALEKV_TRY(check_token_rows(shape, out, chunk, "out"));
   MaskView m;
   SCALEKV_TRY(check_mask(mask, &m));
+  if (out->n_row == 0) return SCALEKV_OK;
   if ((shape->n_head > 1 && out->head_stride < shape->head_dim) || (out->n_row > 1 && out->row_stride < shape->head_dim) ||
       (shape->n_seq > 1 && !chunk->first && out->seq_stride < shape->head_dim))
     return fail(SCALEKV_ERR_INVALID_ARG, "rows of out coincide: a stride is below head_dim");

@@ -111,7 +111,8 @@ __device__ __forceinline__ Slice slice_of(const AttendArgs& a, unsigned wg) {
     const int at = __builtin_ctzll(found);
     first = __builtin_amdgcn_readlane((int)(upto - mine), at);
     s.seq = at * per_lane;
-    for (unsigned n; wg >= first + (n = cutter.workgroups(s.seq)); ++s.seq) first += n;
+    // (the bound holds even if lengths are changed under the call)
+    for (unsigned n; s.seq + 1 < a.n_seq && wg >= first + (n = cutter.workgroups(s.seq)); ++s.seq) first += n;
     s.seq = __builtin_amdgcn_readfirstlane(s.seq);
     first = __builtin_amdgcn_readfirstlane(first);
   }

@@ -228,6 +228,46 @@ def test_two_streams_at_once_and_twice_the_same():
         _check(cache, s, q[s].cpu(), outs[0][s], causal=True)
 
 
+def test_the_binding_refuses_what_does_not_fit_and_says_so():
+    """The calls that native code does not take come to checks that name the argument."""
+    S, H, d, page, dtype = 2, 4, 64, 16, BF16
+    shape, pages = skv.Shape(S, H, d, dtype), P.Cache(1, [20, 30], 2, d, page, E4M3, dtype).on(DEV)
+    q, k = (torch.zeros(S, h, 3, d, dtype=dtype, device=DEV) for h in (H, 2))
+    ws, ints = _workspace(shape, pages, 3), lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    dst = torch.zeros(S, H, 8, d, dtype=dtype, device=DEV)
+    packed = q[0].transpose(0, 1).contiguous()
+    for call, word in (
+            (lambda: skv.pages_write(shape, pages, q, q), "k_new has shape"), (lambda: skv.pages_write(shape, pages, k.float(), k), "dtype"),
+            (lambda: skv.pages_write(shape, pages, k.cpu(), k), "current device"),
+            (lambda: skv.pages_write(shape, pages, k[..., ::2], k), "k_new has shape"),
+            (lambda: skv.pages_write(shape, pages, k, k, count=ints(1)), "count"),
+            (lambda: skv.pages_write(shape, pages, k, k, count=ints(1, 2).long()), "count"),
+            (lambda: skv.pages_write(shape, pages, k, k, max_new=4), "n_row"),
+            (lambda: skv.pages_write(skv.Shape(3, H, d, dtype), pages, k, k), "pages for"),
+            (lambda: skv.pages_read(shape, pages, ints(1), 1, dst, dst.clone()), "idx"),
+            (lambda: skv.pages_read(shape, pages, None, 9, dst, dst.clone()), "capacity"),
+            (lambda: skv.pages_attend(shape, pages, packed, packed.clone(), ws), "max_new is needed"),
+            (lambda: skv.pages_attend(shape, pages, packed, packed.clone(), ws, max_new=3), "first is needed"),
+            (lambda: skv.pages_attend(shape, pages, q, packed, ws), "packed or not"),
+            (lambda: skv.pages_attend(shape, pages, q, q.transpose(2, 3).contiguous().transpose(2, 3), ws), "rows must be contiguous"),
+            (lambda: skv.pages_attend(shape, pages, q, q[:, :1].expand(-1, H, -1, -1), ws), "coincide"),
+            (lambda: skv.Pages(pages.k, pages.v, pages.table, pages.lens), "k_scale"),
+            (lambda: skv.Pages(pages.k, pages.v.transpose(0, 1).contiguous().transpose(0, 1), pages.table, pages.lens,
+                               pages.k_scale, pages.v_scale), "strides"),
+            (lambda: skv.Pages(pages.k, pages.v, pages.table.long(), pages.lens, pages.k_scale, pages.v_scale), "table")):
+        with pytest.raises(skv.ScaleKVError, match=word):
+            call()
+    with pytest.raises(AttributeError):
+        pages.lens = ints(1, 2)
+    skv.pages_check(shape, pages, pages.table.tolist(), [20, 30], max_new=3, n_row=3)
+    with pytest.raises(skv.ScaleKVError, match="len"):
+        skv.pages_check(shape, pages, pages.table.tolist(), [20, 33], max_new=3, n_row=3)
+    # nothing new at all, and a page table of one sequence
+    none = torch.zeros(0, H, d, dtype=dtype, device=DEV)
+    skv.pages_attend(shape, pages, none, none.clone(), ws, first=ints(0, 0), count=ints(0, 0), max_new=3)
+    torch.cuda.synchronize()
+
+
 def _run_all():
     """Every kind of call on fixed inputs: {name: bytes}."""
     got = {"library": os.path.basename(skv.lib_path())}

@@ -200,6 +200,12 @@ def _check(L, table, lens, count=None, first=None, max_new=None, n_row=0, **kw):
                                  ints([x for r in table for x in r]), ints(lens), chunk, ints(first), ints(count), n_row)
 
 
+def test_packed_tensors_without_rows_are_fine(L):
+    none, chunk = _rows(ptr=0, n_row=0, seq_stride=0), _chunk(first=0x7000000, count=0x7100000)
+    assert _write(L, k=none, v=none, chunk=chunk) == OK and _attend(L, q=none, out=none, chunk=chunk) == OK
+    assert _write(L, k=none, v=none) == INVALID                       # (not packed: max_new rows are needed)
+
+
 def test_tables_with_mistakes_are_named(L):
     good = [[0, 1, -1], [2, 9, 5]]
     assert _check(L, good, [40, 96]) == OK                           # (entries behind the last page are not used)
