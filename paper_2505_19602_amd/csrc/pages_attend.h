@@ -56,7 +56,8 @@ __device__ __forceinline__ double wave_sum(double x) {
   x = dpp_add<0x142, 0xa>(x);
   x = dpp_add<0x143, 0xc>(x);
   const unsigned long long bits = __builtin_bit_cast(unsigned long long, x);
-  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)bits, 63), hi = __builtin_amdgcn_readlane((int)(unsigned)(bits >> 32), 63);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)bits, 63);
+  const unsigned hi = __builtin_amdgcn_readlane((int)(unsigned)(bits >> 32), 63);
   return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
 
@@ -67,58 +68,77 @@ __device__ __forceinline__ double wave_sum(double x) {
 struct Slice {
   int seq, kv, row_group, cut, cuts;  // cuts 0: nothing
   int first_wg;                       // of the sequence
+  int len, count;                     // cached rows and new tokens of the sequence
 };
 struct Cutter {
   const AttendArgs& a;
   int tile;   // keys of a tile
   int most;   // tiles to a workgroup
-  __device__ __forceinline__ int groups(int seq) const {
-    return (chunk_count(a.chunk, seq) * a.group + a.rows - 1) / a.rows;
-  }
-  __device__ __forceinline__ int tiles(int seq) const {
-    const int all = (pages_len(a.c, seq) + tile - 1) / tile;
+  __device__ __forceinline__ int groups(int count) const { return (count * a.group + a.rows - 1) / a.rows; }
+  __device__ __forceinline__ int tiles(int len) const {
+    const int all = (len + tile - 1) / tile;
     if (a.mask.window == 0 || !a.mask.causal) return all;
     const int tokens = min(a.chunk.max_new, a.rows / a.group + 1);
     return min(all, (min(a.mask.n_sink, 1 << 29) + tile - 1) / tile + (min(a.mask.window, 1 << 29) + tokens) / tile + 1);
   }
-  __device__ __forceinline__ int cuts(int seq) const { return a.target ? max((tiles(seq) + most - 1) / most, 1) : 1; }
-  __device__ __forceinline__ unsigned workgroups(int seq) const { return (unsigned)(groups(seq) * cuts(seq)) * a.c.n_kv_head; }
+  __device__ __forceinline__ double work(int len, int count) const { return (double)groups(count) * tiles(len); }
+  __device__ __forceinline__ void share(double all) {
+    if (a.target) most = max(a.min_tiles, (int)min(ceil(all * a.c.n_kv_head / a.target), 1e9));
+  }
+  __device__ __forceinline__ int cuts(int len) const { return a.target ? max((tiles(len) + most - 1) / most, 1) : 1; }
+  __device__ __forceinline__ unsigned workgroups(int len, int count) const {
+    return (unsigned)(groups(count) * cuts(len)) * a.c.n_kv_head;
+  }
 };
 template <int TN>
 __device__ __forceinline__ Slice slice_of(const AttendArgs& a, unsigned wg) {
   Cutter cutter{a, TN, 1};
-  const int lane = threadIdx.x & 63, per_lane = (a.n_seq + 63) / 64;
+  const int lane = threadIdx.x & 63;
   Slice s{};
   unsigned first = 0;
+  auto len_of = [&](int seq) { return pages_len(a.c, seq); };
+  auto count_of = [&](int seq) { return chunk_count(a.chunk, seq); };
   if (a.n_seq == 1) {
-    if (a.target) {
-      const double work = (double)cutter.groups(0) * cutter.tiles(0) * a.c.n_kv_head;
-      cutter.most = max(a.min_tiles, (int)min(ceil(work / a.target), 1e9));
-    }
-    if (wg >= cutter.workgroups(0)) return s;
+    s.len = __builtin_amdgcn_readfirstlane(len_of(0));
+    s.count = __builtin_amdgcn_readfirstlane(count_of(0));
+    cutter.share(cutter.work(s.len, s.count));
+    if (wg >= cutter.workgroups(s.len, s.count)) return s;
+  } else if (a.n_seq <= 64) {  // a sequence to a lane, each read once
+    const int len = lane < a.n_seq ? len_of(lane) : 0, count = lane < a.n_seq ? count_of(lane) : 0;
+    if (a.target) cutter.share(wave_sum(cutter.work(len, count)));
+    const unsigned mine = cutter.workgroups(len, count), upto = wave_scan(mine);
+    const unsigned long long found = __builtin_amdgcn_ballot_w64(upto > wg);  // this lane's sequence or earlier ones
+    if (found == 0) return s;
+    s.seq = __builtin_ctzll(found);
+    first = __builtin_amdgcn_readlane((int)(upto - mine), s.seq);
+    s.len = __builtin_amdgcn_readlane(len, s.seq);
+    s.count = __builtin_amdgcn_readlane(count, s.seq);
   } else {
+    const int per_lane = (a.n_seq + 63) / 64, from = lane * per_lane, to = min(from + per_lane, a.n_seq);
     if (a.target) {
       double work = 0;
-      for (int x = lane * per_lane; x < min((lane + 1) * per_lane, a.n_seq); ++x)
-        work += (double)cutter.groups(x) * cutter.tiles(x);
-      cutter.most = max(a.min_tiles, (int)min(ceil(wave_sum(work) * a.c.n_kv_head / a.target), 1e9));
+      for (int x = from; x < to; ++x) work += cutter.work(len_of(x), count_of(x));
+      cutter.share(wave_sum(work));
     }
     unsigned mine = 0;
-    for (int x = lane * per_lane; x < min((lane + 1) * per_lane, a.n_seq); ++x) mine += cutter.workgroups(x);
+    for (int x = from; x < to; ++x) mine += cutter.workgroups(len_of(x), count_of(x));
     const unsigned upto = wave_scan(mine);
-    const unsigned long long found = __builtin_amdgcn_ballot_w64(upto > wg);  // this lane's sequences or earlier ones
+    const unsigned long long found = __builtin_amdgcn_ballot_w64(upto > wg);
     if (found == 0) return s;
     const int at = __builtin_ctzll(found);
     first = __builtin_amdgcn_readlane((int)(upto - mine), at);
     s.seq = at * per_lane;
     // (the bound holds even if lengths are changed under the call)
-    for (unsigned n; s.seq + 1 < a.n_seq && wg >= first + (n = cutter.workgroups(s.seq)); ++s.seq) first += n;
+    for (unsigned n; s.seq + 1 < a.n_seq && wg >= first + (n = cutter.workgroups(len_of(s.seq), count_of(s.seq))); ++s.seq)
+      first += n;
     s.seq = __builtin_amdgcn_readfirstlane(s.seq);
     first = __builtin_amdgcn_readfirstlane(first);
+    s.len = __builtin_amdgcn_readfirstlane(len_of(s.seq));
+    s.count = __builtin_amdgcn_readfirstlane(count_of(s.seq));
   }
   s.first_wg = (int)first;
-  s.cuts = __builtin_amdgcn_readfirstlane(cutter.cuts(s.seq));
-  const int n_group = __builtin_amdgcn_readfirstlane(cutter.groups(s.seq)), per = n_group * s.cuts;
+  s.cuts = __builtin_amdgcn_readfirstlane(cutter.cuts(s.len));
+  const int n_group = cutter.groups(s.count), per = n_group * s.cuts;
   // Eight heads at a time, dealt out in turn: consecutive workgroups go round-robin over the XCDs, so that the workgroups
   // of a head share an L2.
   const int heads = a.c.n_kv_head, dealt = heads / kXcds * kXcds;
@@ -162,9 +182,9 @@ struct Seen {
   int plain_begin, plain_end;    // every row sees all of these tiles
   __device__ __forceinline__ int end_of(int p) const { return causal ? min(len, p + 1) : len; }
   __device__ __forceinline__ int begin_of(int p) const { return window ? p - width + 1 : -0x7fffffff; }
-  __device__ __forceinline__ Seen(const AttendArgs& a, int seq, int first_row, int rows) {
-    len = __builtin_amdgcn_readfirstlane(pages_len(a.c, seq));  // (all of this is the same in every lane: scalars)
-    count = __builtin_amdgcn_readfirstlane(chunk_count(a.chunk, seq));
+  __device__ __forceinline__ Seen(const AttendArgs& a, const Slice& slice, int first_row, int rows) {
+    len = slice.len;  // (all of this is the same in every lane: scalars)
+    count = slice.count;
     n_rows = count * a.group;
     pos0 = len - count;
     causal = a.mask.causal;
@@ -268,7 +288,8 @@ __device__ __forceinline__ float cached_value(const unsigned char* pool, const u
 // a weight of zero would make NaN of them): this adds them, for the rows that see them, to the sums of a wave.  The sums
 // are in LDS meanwhile (rows of D fp32, this wave's alone), so that nothing of this is held through the tile loop.  neg: less
 // the offset of row 16 b + i, in lanes 16 g + i.  Keys [from, to) of each such tile in [t0, t1) are looked at: those
-// that the wave has worked on, whose offsets are no lower than their logits.  Rare, and written to be short: the logits are formed anew, a channel at a time.
+// that the wave has worked on, whose offsets are no lower than their logits.  Rare, and written to be short: the logits are
+// formed anew, a channel at a time.
 template <int TYPE, bool Q8, int D, int TN, int RT>
 __device__ __forceinline__ void add_odd(const AttendArgs& a, const Seen<TN>& seen, int seq, int kv, int wave_row, int t0,
                                         int t1, int from, int to, const float (&neg)[RT], float* sums) {
@@ -323,28 +344,25 @@ __device__ __forceinline__ void add_odd(const AttendArgs& a, const Seen<TN>& see
   }
 }
 
-// The sums of a wave (o: channels 16 c + 4 g + v of row 16 b + i, lane 16 g + i) through LDS and back, for add_odd().
-template <int D, int RT>
-__device__ __forceinline__ void sums_to_lds(const f32x4 (&o)[RT][D / 16], float* sums) {
-  const int i = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
-#pragma unroll
-  for (int b = 0; b < RT; ++b)
-#pragma unroll
-    for (int x = 0; x < D / 16; ++x) *(f32x4*)(sums + (16 * b + i) * D + 16 * x + 4 * g) = o[b][x];
+// Sixteen rows of a wave's sums (o: channels 16 c + 4 g + v of row i, lane 16 g + i) through LDS and back, for add_odd().
+__device__ __forceinline__ void own_lds() {  // the wave's own stores have landed
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the wave's own stores have landed
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-template <int D, int RT>
-__device__ __forceinline__ void sums_from_lds(f32x4 (&o)[RT][D / 16], const float* sums) {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+template <int D>
+__device__ __forceinline__ void sums_to_lds(const f32x4 (&o)[D / 16], float* sums) {
   const int i = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
 #pragma unroll
-  for (int b = 0; b < RT; ++b)
+  for (int x = 0; x < D / 16; ++x) *(f32x4*)(sums + i * D + 16 * x + 4 * g) = o[x];
+  own_lds();
+}
+template <int D>
+__device__ __forceinline__ void sums_from_lds(f32x4 (&o)[D / 16], const float* sums) {
+  own_lds();
+  const int i = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
 #pragma unroll
-    for (int x = 0; x < D / 16; ++x) o[b][x] = *(const f32x4*)(sums + (16 * b + i) * D + 16 * x + 4 * g);
+  for (int x = 0; x < D / 16; ++x) o[x] = *(const f32x4*)(sums + i * D + 16 * x + 4 * g);
 }
 
 }  // namespace scalekv

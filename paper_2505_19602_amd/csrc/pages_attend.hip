@@ -6,18 +6,26 @@
 // the group) in this order, so that the heads that share a row of the cache read it together: a single token of a group of
 // eight heads is eight rows.
 //
+// Here: up to 16 rows to a workgroup (single tokens, short chunks), and fp32; many rows of bf16 are pages_chunk.hip's.
+//
 // Products, transposed as in the dense kernels: S^T[key][row] = K Q^T with K from LDS and Q in registers, O^T[channel][row]
-// += V^T P^T with V^T from LDS and P^T in the registers that the first product left it in; a lane owns a query row (of each
-// tile of 16), its softmax statistics are scalars of the lane.  bf16: MFMA 16x16x32, blocks of 32 keys, key order and LDS
-// swizzle as in attend_pipe.hip.  fp32: MFMA 16x16x4, blocks of 16 keys.
+// += V^T P^T with V^T from LDS and P^T in the registers that the first product left it in; a lane owns a query row, its
+// softmax statistics are scalars of the lane.  bf16: MFMA 16x16x32, blocks of 32 keys, key order and LDS swizzle as in
+// attend_pipe.hip.  fp32: MFMA 16x16x4, blocks of 16 keys.
 //
 // Tiles.  All waves bring in a tile of keys: whole rows, 16 bytes a lane, through registers into LDS, where e4m3 becomes
 // what the products take (exactly: four significant bits and a power of two), rows that no query row of the workgroup sees
 // become zeros, and the rows of the tile after it are requested before this one is worked on, their pages' numbers one
-// tile earlier still.  Waves either split the query rows (chunks) or the blocks of a tile (few rows), and in the latter
-// case join their results through LDS.  Where that leaves the chip idle the keys are split over workgroups as well; their
-// results go to the workspace, and pages_join_kernel adds them up.  A workgroup walks the tiles that its rows can see:
-// those of the first rows, then those from the window's first row on.
+// tile earlier still.  Waves split the blocks of a tile and join their results through LDS (fp32 with many rows: they split
+// the rows).  Where that leaves the chip idle the keys are split over workgroups as well; their results go to the
+// workspace, and pages_join_kernel adds them up.  A workgroup walks the tiles that its rows can see: those of the first
+// rows, then those from the window's first row on.
+//
+// What bounds it.  Few rows: HBM, each cached row being read once.  8 KV heads, head_dim 128, one token of 4 heads each: 64
+// sequences x 8000 rows bf16 361 us (5.8 TB/s), e4m3 194 us (5.5 TB/s); 2 x 131072 rows bf16 191 us (5.6 TB/s), e4m3 111 us; 64
+// sequences of up to 4000 rows, e4m3, 78 us (3.7 TB/s: the shortest workgroups are all start and end).  Small calls: the
+// chain length -> table -> rows -> products, and the join's launch: one sequence of 700 rows 10 us.  fp32, many rows: the
+// fp32 matrix rate, 24 units x 2048 causal tokens, head_dim 128, 411 us (63 TFLOP/s; a large product reaches 154).
 //
 // Masked keys.  A weight of zero does not hide a value that is infinite or NaN from the product.  Rows hidden from all rows
 // of the workgroup are zeros in LDS; in the few tiles that some of its rows see and others do not (`edge`), values that
@@ -31,33 +39,33 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// TYPE: of queries, output and arithmetic; WQ: waves that split the query rows; RT: tiles of 16 query rows to a wave.
-template <int TYPE, bool Q8, int D, int WQ, int RT>
+// TYPE: of queries, output and arithmetic; WQ: waves that split the query rows, 16 to each.
+template <int TYPE, bool Q8, int D, int WQ>
 struct Form {
+  static_assert(TYPE == kTypeF32 || WQ == 1, "many rows of bf16 are pages_chunk.hip's");
   static constexpr bool kBf16 = TYPE == kTypeBf16;
   static constexpr int kElem = kBf16 ? 2 : 4;
   static constexpr int WK = 4 / WQ;                      // waves that split the keys of a tile
   static constexpr int kBlock = kBf16 ? 32 : 16;         // keys of a block
-  static constexpr int kBlocks = WK > 1 ? 1 : kBf16 ? 2 : 4;  // blocks of a tile to a wave
+  static constexpr int kBlocks = WK > 1 ? 1 : 4;         // blocks of a tile to a wave
   static constexpr int TN = kBlock * kBlocks * WK;       // keys of a tile
   static constexpr int kKeyTiles = kBlock / 16;
   static constexpr int kRowBytes = D * kElem;            // in LDS
   static constexpr int kTileBytes = TN * kRowBytes;
   // Keys in LDS as codes, widened where a wave takes them: only that wave does, and three workgroups fit a compute unit
-  // instead of two
-  static constexpr bool kKeyCodes = kBf16 && Q8 && WK > 1;
+  // instead of two (with cuts by the work of all sequences, 16 units x 131072 rows e4m3 160 -> 113 us)
+  static constexpr bool kKeyCodes = kBf16 && Q8;
   static constexpr int kKeyTileBytes = kKeyCodes ? TN * D : kTileBytes;
-  static constexpr int kStages = WK == 1 && kBf16 ? 2 : 1;
   static constexpr int kSlabs = kRowBytes / 64;          // 16-byte operands of a query row that a lane holds
   static constexpr int kChans = D / 16;                  // 16-channel blocks of the output
   static constexpr int kSrcRow = Q8 ? D : kRowBytes;     // bytes of a cached row
   static constexpr int kSrcChunks = kSrcRow / 16;
   static constexpr int kVecs = TN * kSrcChunks / kThreads;  // 16-byte vectors of a tile of K, or of V, to a thread
-  static constexpr int kRows = 16 * RT * WQ;             // query rows of a workgroup
-  static constexpr int kWavesPerSimd = kKeyCodes && RT == 1 ? 3 : 2;
-  static constexpr int kJoinBytes = WK > 1 ? (WK - 1) * 64 * RT * (kChans * 16 + 8) : 0;
-  static constexpr int kSumBytes = 4 * 16 * RT * D * 4;  // of all waves, for add_odd()
-  static constexpr int kTilesBytes = kStages * (kKeyTileBytes + kTileBytes);
+  static constexpr int kRows = 16 * WQ;                  // query rows of a workgroup
+  static constexpr int kWavesPerSimd = kKeyCodes ? 3 : 2;
+  static constexpr int kJoinBytes = WK > 1 ? (WK - 1) * 64 * (kChans * 16 + 8) : 0;
+  static constexpr int kSumBytes = 4 * 16 * D * 4;  // of all waves, for add_odd()
+  static constexpr int kTilesBytes = kKeyTileBytes + kTileBytes;
   static constexpr int kLds = kTilesBytes > kJoinBytes ? kTilesBytes > kSumBytes ? kTilesBytes : kSumBytes
                                                        : kJoinBytes > kSumBytes ? kJoinBytes : kSumBytes;
   __device__ static constexpr int k_flip(int r) { return kBf16 ? k_flip_bf16<D>(r) : r & 15; }
@@ -69,9 +77,10 @@ struct Form {
   }
 };
 
-template <int TYPE, bool Q8, int D, int WQ, int RT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<TYPE, Q8, D, WQ, RT>::kWavesPerSimd))) void pages_attend_kernel(AttendArgs a) {
-  using F = Form<TYPE, Q8, D, WQ, RT>;
+template <int TYPE, bool Q8, int D, int WQ>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<TYPE, Q8, D, WQ>::kWavesPerSimd)))
+void pages_attend_kernel(AttendArgs a) {
+  using F = Form<TYPE, Q8, D, WQ>;
   constexpr bool BF16 = F::kBf16;
   constexpr int TN = F::TN, KT = F::kKeyTiles, NSL = F::kSlabs, NCB = F::kChans, NV = F::kVecs;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -87,31 +96,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wq = wave % WQ, wk = wave / WQ;
-  const int first_row = slice.row_group * F::kRows, wave_row = first_row + wq * (16 * RT);
-  const Seen<TN> seen(a, seq, first_row, F::kRows);
+  const int first_row = slice.row_group * F::kRows, wave_row = first_row + wq * 16;
+  const Seen<TN> seen(a, slice, first_row, F::kRows);
   const int n_rows = seen.n_rows, pos0 = seen.pos0, sinks = seen.sinks;
   const int per = (seen.n_tile + slice.cuts - 1) / slice.cuts;
   const int t0 = min(slice.cut * per, seen.n_tile), t1 = min(t0 + per, seen.n_tile);
 
   // ---- the query rows of this lane
-  int q_end[RT], q_begin[RT], q_row[RT];
-  u32x4 qf[RT][NSL];
-#pragma unroll
-  for (int b = 0; b < RT; ++b) {
-    const int r = min(wave_row + 16 * b + i, n_rows - 1);
-    const int t = r / a.group, head = kv * a.group + (r - t * a.group);
-    q_row[b] = r;
-    q_end[b] = seen.end_of(pos0 + t);
-    q_begin[b] = seen.begin_of(pos0 + t);
+  const int q_row = min(wave_row + i, n_rows - 1);
+  int q_end, q_begin;
+  u32x4 qf[NSL];
+  {
+    const int t = q_row / a.group, head = kv * a.group + (q_row - t * a.group);
+    q_end = seen.end_of(pos0 + t);
+    q_begin = seen.begin_of(pos0 + t);
     const long long at = (long long)chunk_first(a.chunk, seq) + t;
     const u32x4* src = (const u32x4*)(a.q.p + seq * a.q.seq + head * a.q.head + at * a.q.row);
     const bool there = at >= 0 && at < a.q.n_row;
 #pragma unroll
-    for (int sl = 0; sl < NSL; ++sl) qf[b][sl] = there ? src[4 * sl + g] : u32x4{0, 0, 0, 0};
+    for (int sl = 0; sl < NSL; ++sl) qf[sl] = there ? src[4 * sl + g] : u32x4{0, 0, 0, 0};
   }
   // what all rows of the wave see: [begin, end) and the first `sinks`
   const int w_end = seen.end_of(pos0 + min(wave_row, n_rows - 1) / a.group);
-  const int w_begin = seen.begin_of(pos0 + min(wave_row + 16 * RT - 1, n_rows - 1) / a.group);
+  const int w_begin = seen.begin_of(pos0 + min(wave_row + 15, n_rows - 1) / a.group);
 
   // ---- tiles: a thread's vectors of a tile lie kThreads vectors apart
   int page[NV];
@@ -149,9 +156,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       }
     }
   };
-  auto store_rows = [&](int t, int stage) __attribute__((always_inline)) {
-    unsigned char* const k_lds = smem + stage * F::kKeyTileBytes;
-    unsigned char* const v_lds = smem + F::kStages * F::kKeyTileBytes + stage * F::kTileBytes;
+  unsigned char* const k_lds = smem;
+  unsigned char* const v_lds = smem + F::kKeyTileBytes;
+  auto store_rows = [&](int t) __attribute__((always_inline)) {
     const bool edge = seen.edge(t);
     constexpr int kOut = Q8 ? F::kElem : 1;  // vectors in LDS for one of the cache
 #pragma unroll
@@ -186,24 +193,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   };
 
   // ---- state of the rows
-  f32x4 o[RT][NCB];
+  f32x4 o[NCB];
   // Less the offset of a row, its largest logit in log2 units (the same in the four lanes of a row), and this lane's share of
   // the sum.  The offset is kept as it has been rounded: factors between offsets are then exactly those between the weights
   // (formed from the logits anew they are off by the rounding of the product, 2^-24 of its magnitude).
-  float neg[RT], l_run[RT];
+  float neg = -(a.no_max * a.scale_log2e), l_run = 0.f;
 #pragma unroll
-  for (int b = 0; b < RT; ++b) {
-#pragma unroll
-    for (int x = 0; x < NCB; ++x) o[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    neg[b] = -(a.no_max * a.scale_log2e);
-    l_run[b] = 0.f;
-  }
+  for (int x = 0; x < NCB; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
   // key of register v of key tile t, in a block
   auto key_of = [&](int t, int v) { return BF16 ? 16 * (g & 1) + 8 * (g >> 1) + 4 * t + v : 4 * g + v; };
 
-  auto work = [&](int t, int stage) __attribute__((always_inline)) {
-    const unsigned char* const k_lds = smem + stage * F::kKeyTileBytes;
-    const unsigned char* const v_lds = smem + F::kStages * F::kKeyTileBytes + stage * F::kTileBytes;
+  auto work = [&](int t) __attribute__((always_inline)) {
     const int key0 = seen.key0(t);
     const bool masked = key0 + TN > w_end || (seen.window && key0 < w_begin && key0 + TN > sinks);
 #pragma unroll 1  // (blocks side by side spill registers)
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       const int block = wk * F::kBlocks + nb;
       const unsigned char* const kb = k_lds + block * F::kBlock * (F::kKeyCodes ? D : F::kRowBytes);
       const unsigned char* const vb = v_lds + block * F::kBlock * F::kRowBytes;
-      f32x4 s[RT][KT];
+      f32x4 s[KT];
 #pragma unroll
       for (int x = 0; x < KT; ++x) {
         const int row = BF16 ? 16 * (i >> 2 & 1) + 8 * (i >> 3) + (i & 3) + 4 * x : i;
@@ -222,35 +222,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
             const uint2 codes = *(const uint2*)(kb + row * D + 16 * ((2 * sl + g / 2) ^ F::code_flip(row)) + 8 * (g & 1));
             const float scale = __uint_as_float((unsigned)key_scale[block * F::kBlock + row] << 23);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              kf[sl][e] = __builtin_bit_cast(unsigned, e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e < 2 ? codes.x : codes.y, scale, true)
-                                                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e < 2 ? codes.x : codes.y, scale, false));
+            for (int e = 0; e < 4; ++e) {
+              const unsigned four = e < 2 ? codes.x : codes.y;
+              const bf16x2 two = e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true)
+                                       : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, false);
+              kf[sl][e] = __builtin_bit_cast(unsigned, two);
+            }
           } else {
             kf[sl] = *(const u32x4*)(kb + row * F::kRowBytes + 16 * ((4 * sl + g) ^ F::k_flip(row)));
           }
         }
         if constexpr (BF16) {
+          s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int b = 0; b < RT; ++b) s[b][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int sl = 0; sl < NSL; ++sl)
+            s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sl]),
+                                                           __builtin_bit_cast(bf16x8, qf[sl]), s[x], 0, 0, 0);
+        } else {
+          // four sums of every fourth channel: shorter chains, of instructions and of roundings
+          f32x4 sum[4];
 #pragma unroll
           for (int sl = 0; sl < NSL; ++sl)
 #pragma unroll
-            for (int b = 0; b < RT; ++b)
-              s[b][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sl]),
-                                                                __builtin_bit_cast(bf16x8, qf[b][sl]), s[b][x], 0, 0, 0);
-        } else {
-          // four sums of every fourth channel: shorter chains, of instructions and of roundings
-#pragma unroll
-          for (int b = 0; b < RT; ++b) {
-            f32x4 sum[4];
-#pragma unroll
-            for (int sl = 0; sl < NSL; ++sl)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                sum[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sl][e]), __uint_as_float(qf[b][sl][e]),
-                                                              sl ? sum[e] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            s[b][x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          }
+            for (int e = 0; e < 4; ++e)
+              sum[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sl][e]), __uint_as_float(qf[sl][e]),
+                                                            sl ? sum[e] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          s[x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
       }
       if (masked) {
@@ -259,52 +256,37 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const int pos = key0 + block * F::kBlock + key_of(x, v);
-#pragma unroll
-            for (int b = 0; b < RT; ++b)
-              if (pos >= q_end[b] || (pos < q_begin[b] && pos >= sinks)) s[b][x][v] = -INFINITY;
+            if (pos >= q_end || (pos < q_begin && pos >= sinks)) s[x][v] = -INFINITY;
           }
       }
       // Running maximum, moved only where it has grown by more than kRescaleThreshold; in fp32 wherever it has grown, so that
       // the exponents of the weights that count are small, and with them the rounding of an exponent.
-      float mx[RT];
-      bool grow = false;
+      float mx = s[0][0];
 #pragma unroll
-      for (int b = 0; b < RT; ++b) {
-        float m = s[b][0][0];
+      for (int y = 1; y < 4 * KT; ++y) mx = fmaxf(mx, s[y / 4][y % 4]);
+      mx = xor32_max(xor16_max(mx));
+      if (__builtin_amdgcn_ballot_w64(fmaf(mx, a.scale_log2e, neg) > (BF16 ? kRescaleThreshold : 0.f)) != 0) {
+        const float now = fminf(neg, -(mx * a.scale_log2e)), alpha = __builtin_amdgcn_exp2f(now - neg);
+        neg = now;
+        l_run *= alpha;
 #pragma unroll
-        for (int y = 1; y < 4 * KT; ++y) m = fmaxf(m, s[b][y / 4][y % 4]);
-        mx[b] = xor32_max(xor16_max(m));
-        grow |= fmaf(mx[b], a.scale_log2e, neg[b]) > (BF16 ? kRescaleThreshold : 0.f);
+        for (int x = 0; x < NCB; ++x) o[x] *= alpha;
       }
-      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+      float w[4 * KT];
+      u32x4 p;
 #pragma unroll
-        for (int b = 0; b < RT; ++b) {
-          const float now = fminf(neg[b], -(mx[b] * a.scale_log2e));
-          const float alpha = __builtin_amdgcn_exp2f(now - neg[b]);
-          neg[b] = now;
-          l_run[b] *= alpha;
+      for (int y = 0; y < 4 * KT; ++y) w[y] = __builtin_amdgcn_exp2f(fmaf(s[y / 4][y % 4], a.scale_log2e, neg));
+      if constexpr (BF16) {
+        // (weights are rounded to bf16 for the matrix cores; the sum adds the rounded ones)
 #pragma unroll
-          for (int x = 0; x < NCB; ++x) o[b][x] *= alpha;
+        for (int y = 0; y < 4; ++y) {
+          const bf16x2 two = {(__bf16)w[2 * y], (__bf16)w[2 * y + 1]}, ones = {(__bf16)1.f, (__bf16)1.f};
+          l_run = __builtin_amdgcn_fdot2_f32_bf16(two, ones, l_run, false);
+          p[y] = __builtin_bit_cast(unsigned, two);
         }
-      }
-      float w[RT][4 * KT];
-      u32x4 p[RT];
+      } else {
 #pragma unroll
-      for (int b = 0; b < RT; ++b) {
-#pragma unroll
-        for (int y = 0; y < 4 * KT; ++y) w[b][y] = __builtin_amdgcn_exp2f(fmaf(s[b][y / 4][y % 4], a.scale_log2e, neg[b]));
-        if constexpr (BF16) {
-          // (weights are rounded to bf16 for the matrix cores; the sum adds the rounded ones)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const bf16x2 two = {(__bf16)w[b][2 * y], (__bf16)w[b][2 * y + 1]}, ones = {(__bf16)1.f, (__bf16)1.f};
-            l_run[b] = __builtin_amdgcn_fdot2_f32_bf16(two, ones, l_run[b], false);
-            p[b][y] = __builtin_bit_cast(unsigned, two);
-          }
-        } else {
-#pragma unroll
-          for (int y = 0; y < 4 * KT; ++y) l_run[b] += w[b][y];
-        }
+        for (int y = 0; y < 4 * KT; ++y) l_run += w[y];
       }
 #pragma unroll
       for (int ch = 0; ch < NCB; ++ch) {
@@ -315,16 +297,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
           const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
           const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * F::kRowBytes));
           const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int b = 0; b < RT; ++b)
-            o[b][ch] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, p[b]), o[b][ch], 0, 0, 0);
+          o[ch] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, p), o[ch], 0, 0, 0);
         } else {
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const int row = 4 * g + v;
-            const float val = *(const float*)(vb + row * F::kRowBytes + 16 * ((4 * ch + (i >> 2)) ^ F::v_flip(row)) + 4 * (i & 3));
-#pragma unroll
-            for (int b = 0; b < RT; ++b) o[b][ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(val, w[b][v], o[b][ch], 0, 0, 0);
+            const int chunk = (4 * ch + (i >> 2)) ^ F::v_flip(row);
+            const float val = *(const float*)(vb + row * F::kRowBytes + 16 * chunk + 4 * (i & 3));
+            o[ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(val, w[v], o[ch], 0, 0, 0);
           }
         }
       }
@@ -338,99 +318,85 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     ask_rows(t0);
     ask_pages(t0 + 1);
     __syncthreads();
-    store_rows(t0, 0);
+    store_rows(t0);
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-      const int stage = F::kStages > 1 ? (t - t0) & 1 : 0;
       if (t + 1 < t1) {
         ask_rows(t + 1);
         ask_pages(t + 2);
       }
-      if (wave_row < n_rows) work(t, stage);  // (the others only carry their share of the tiles)
-      if constexpr (F::kStages > 1) {
-        if (t + 1 < t1) store_rows(t + 1, stage ^ 1);  // (left by all waves before the last barrier)
-      } else {
-        __syncthreads();
-        if (t + 1 < t1) store_rows(t + 1, 0);
-      }
+      if (wave_row < n_rows) work(t);  // (the others only carry their share of the tiles)
+      __syncthreads();
+      if (t + 1 < t1) store_rows(t + 1);
       __syncthreads();
     }
     if (any_odd && wave_row < n_rows) {
-      float* const sums = (float*)smem + wave * (16 * RT * D);
-      sums_to_lds<D, RT>(o, sums);
+      float* const sums = (float*)smem + wave * (16 * D);
+      sums_to_lds<D>(o, sums);
       constexpr int kMine = F::kBlocks * F::kBlock;
-      add_odd<TYPE, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t1, wk * kMine, (wk + 1) * kMine, neg, sums);
-      sums_from_lds<D, RT>(o, sums);
+      const float less[1] = {neg};
+      add_odd<TYPE, Q8, D, TN, 1>(a, seen, seq, kv, wave_row, t0, t1, wk * kMine, (wk + 1) * kMine, less, sums);
+      sums_from_lds<D>(o, sums);
     }
   }
 
   // ---- join the waves that have split the keys: a common maximum, then the sums
-#pragma unroll
-  for (int b = 0; b < RT; ++b) l_run[b] = xor32_sum(xor16_sum(l_run[b]));
+  l_run = xor32_sum(xor16_sum(l_run));
   if constexpr (F::WK > 1) {
-    f32x4* const part = (f32x4*)smem;                                     // [wave - 1][b][channel block][lane]
-    float* const stat = (float*)(smem + (F::WK - 1) * RT * NCB * 64 * 16);  // [wave - 1][b][2][lane]
+    f32x4* const part = (f32x4*)smem;                                  // [wave - 1][channel block][lane]
+    float* const stat = (float*)(smem + (F::WK - 1) * NCB * 64 * 16);  // [wave - 1][2][lane]
     __syncthreads();
     if (wk > 0) {
 #pragma unroll
-      for (int b = 0; b < RT; ++b) {
-#pragma unroll
-        for (int ch = 0; ch < NCB; ++ch) part[(((wk - 1) * RT + b) * NCB + ch) * 64 + lane] = o[b][ch];
-        stat[(((wk - 1) * RT + b) * 2) * 64 + lane] = neg[b];
-        stat[(((wk - 1) * RT + b) * 2 + 1) * 64 + lane] = l_run[b];
-      }
+      for (int ch = 0; ch < NCB; ++ch) part[((wk - 1) * NCB + ch) * 64 + lane] = o[ch];
+      stat[(wk - 1) * 128 + lane] = neg;
+      stat[(wk - 1) * 128 + 64 + lane] = l_run;
     }
     __syncthreads();
     if (wk > 0) return;
+    float now = neg;
 #pragma unroll
-    for (int b = 0; b < RT; ++b) {
-      float now = neg[b];
+    for (int x = 0; x < F::WK - 1; ++x) now = fminf(now, stat[x * 128 + lane]);
+    const float own = __builtin_amdgcn_exp2f(now - neg);
+    l_run *= own;
 #pragma unroll
-      for (int x = 0; x < F::WK - 1; ++x) now = fminf(now, stat[((x * RT + b) * 2) * 64 + lane]);
-      const float own = __builtin_amdgcn_exp2f(now - neg[b]);
-      l_run[b] *= own;
+    for (int ch = 0; ch < NCB; ++ch) o[ch] *= own;
 #pragma unroll
-      for (int ch = 0; ch < NCB; ++ch) o[b][ch] *= own;
+    for (int x = 0; x < F::WK - 1; ++x) {
+      const float f = __builtin_amdgcn_exp2f(now - stat[x * 128 + lane]);
+      l_run += f * stat[x * 128 + 64 + lane];
 #pragma unroll
-      for (int x = 0; x < F::WK - 1; ++x) {
-        const float f = __builtin_amdgcn_exp2f(now - stat[((x * RT + b) * 2) * 64 + lane]);
-        l_run[b] += f * stat[((x * RT + b) * 2 + 1) * 64 + lane];
-#pragma unroll
-        for (int ch = 0; ch < NCB; ++ch) o[b][ch] += f * part[((x * RT + b) * NCB + ch) * 64 + lane];
-      }
-      neg[b] = now;
+      for (int ch = 0; ch < NCB; ++ch) o[ch] += f * part[(x * NCB + ch) * 64 + lane];
     }
+    neg = now;
   }
 
   // ---- write
-#pragma unroll
-  for (int b = 0; b < RT; ++b) {
-    if (wave_row + 16 * b + i >= n_rows) continue;
-    const int r = q_row[b], t = r / a.group, head = kv * a.group + (r - t * a.group);
-    if (slice.cuts > 1) {
-      const long long row = (long long)wg * a.part_rows + (r - first_row);
-      if (g == 0) {
-        a.stat[2 * row] = -neg[b];
-        a.stat[2 * row + 1] = l_run[b];
-      }
-#pragma unroll
-      for (int ch = 0; ch < NCB; ++ch) *(f32x4*)(a.part + row * D + 16 * ch + 4 * g) = o[b][ch];
-      continue;
+  if (wave_row + i >= n_rows) return;
+  if (slice.cuts > 1) {
+    const long long row = (long long)wg * a.part_rows + (q_row - first_row);
+    if (g == 0) {
+      a.stat[2 * row] = -neg;
+      a.stat[2 * row + 1] = l_run;
     }
-    const long long at = (long long)chunk_first(a.chunk, seq) + t;
-    if (at < 0 || at >= a.out.n_row) continue;
-    // a row that sees nothing, or keys of weight zero only, is zero
-    const float inv = l_run[b] == 0.f ? 0.f : 1.f / l_run[b];
-    unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
 #pragma unroll
-    for (int ch = 0; ch < NCB; ++ch) {
-      const f32x4 x = l_run[b] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[b][ch] * inv;
-      if constexpr (BF16) {
-        const bf16x2 lo2 = {(__bf16)x[0], (__bf16)x[1]}, hi2 = {(__bf16)x[2], (__bf16)x[3]};
-        *(uint2*)(dst + 32 * ch + 8 * g) = make_uint2(__builtin_bit_cast(unsigned, lo2), __builtin_bit_cast(unsigned, hi2));
-      } else {
-        *(f32x4*)(dst + 64 * ch + 16 * g) = x;
-      }
+    for (int ch = 0; ch < NCB; ++ch) *(f32x4*)(a.part + row * D + 16 * ch + 4 * g) = o[ch];
+    return;
+  }
+  const int t = q_row / a.group, head = kv * a.group + (q_row - t * a.group);
+  const long long at = (long long)chunk_first(a.chunk, seq) + t;
+  if (at < 0 || at >= a.out.n_row) return;
+  // a row that sees nothing, or keys of weight zero only, is zero
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  unsigned char* const dst = a.out.p + seq * a.out.seq + head * a.out.head + at * a.out.row;
+#pragma unroll
+  for (int ch = 0; ch < NCB; ++ch) {
+    const f32x4 x = l_run == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[ch] * inv;
+    if constexpr (BF16) {
+      const bf16x2 lo2 = {(__bf16)x[0], (__bf16)x[1]}, hi2 = {(__bf16)x[2], (__bf16)x[3]};
+      *(uint2*)(dst + 32 * ch + 8 * g) = make_uint2(__builtin_bit_cast(unsigned, lo2), __builtin_bit_cast(unsigned, hi2));
+    } else {
+      *(f32x4*)(dst + 64 * ch + 16 * g) = x;
     }
   }
 }
@@ -484,13 +450,13 @@ __global__ __launch_bounds__(kThreads) void pages_join_kernel(AttendArgs a, int 
   }
 }
 
-template <int TYPE, bool Q8, int D, int WQ, int RT>
+template <int TYPE, bool Q8, int D, int WQ>
 hipError_t launch_form(const AttendArgs& a, int n_wg, hipStream_t stream) {
-  using F = Form<TYPE, Q8, D, WQ, RT>;
+  using F = Form<TYPE, Q8, D, WQ>;
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = allow_dynamic_lds((const void*)pages_attend_kernel<TYPE, Q8, D, WQ, RT>, F::kLds, done);
+  const hipError_t e = allow_dynamic_lds((const void*)pages_attend_kernel<TYPE, Q8, D, WQ>, F::kLds, done);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((pages_attend_kernel<TYPE, Q8, D, WQ, RT>), dim3(n_wg), dim3(kThreads), F::kLds, stream, a);
+  hipLaunchKernelGGL((pages_attend_kernel<TYPE, Q8, D, WQ>), dim3(n_wg), dim3(kThreads), F::kLds, stream, a);
   return hipGetLastError();
 }
 
@@ -498,9 +464,10 @@ template <int TYPE, bool Q8, int D>
 hipError_t launch_plan(const PagesPlan& plan, const AttendArgs& a, hipStream_t stream) {
   if constexpr (TYPE == kTypeBf16) {
     if (plan.row_waves == 4) return launch_pages_chunk(D, Q8, plan.row_tiles, a, plan.n_wg, stream);
-    return plan.row_tiles == 2 ? launch_form<TYPE, Q8, D, 1, 2>(a, plan.n_wg, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, plan.n_wg, stream);
+    return launch_form<TYPE, Q8, D, 1>(a, plan.n_wg, stream);
   } else {
-    return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4, 1>(a, plan.n_wg, stream) : launch_form<TYPE, Q8, D, 1, 1>(a, plan.n_wg, stream);
+    return plan.row_waves == 4 ? launch_form<TYPE, Q8, D, 4>(a, plan.n_wg, stream)
+                               : launch_form<TYPE, Q8, D, 1>(a, plan.n_wg, stream);
   }
 }
 
@@ -517,28 +484,41 @@ PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& p
     const long long seen = (long long)mask.n_sink + mask.window + max_new;
     keys = seen < cap ? seen : cap;
   }
-  // The fewest rows that hold a unit's, up to 128 (fp32: 16 or 64), and fewer where that leaves compute units without work
-  // that the keys, cut into pieces of min_tiles tiles, do not give them either.
+  // Rows of a workgroup.  Keys that 64 or 128 rows share are read once for them and their products fill the matrix cores; 16
+  // rows leave more workgroups, whose waves split the keys.  A form is taken for units of more than `over` rows.  us with 16 /
+  // 64 / 128 rows to a workgroup, 128 units x 2000 rows of the cache, head_dim 128: bf16, units of 16 rows 38 / 34 / 41, 32 rows
+  // 42 / 39 / 46, 64 rows 56 / 41 / 48, 128 rows 103 / 49 / 54, 256 rows 189 / 79 / 69; e4m3, 32 rows 35 / 46 / 54, 48 rows 40 /
+  // 47 / 56, 64 rows 46 / 48 / 56, 128 rows 77 / 56 / 61, 256 rows 128 / 95 / 74.  (The form of 16 rows has the shortest start:
+  // 16 units of 4 rows x 2000 12.5 / 25 / 33.)  fp32, 16 / 64 rows, head_dim 64: 192 units x 2000 rows, 32 rows 68 / 120, 64 rows
+  // 105 / 125, 145 rows 254 / 260; 96 units of 1024 rows x 4000 1386 / 1048.
+  // Fewer rows, too, where compute units would be left without work and the keys, in pieces of min_tiles tiles, do not give
+  // them any: bf16, 16 units x 6000 rows, 32 rows 28 / 37 / 46, 256 rows 73 / 45 / 50; fp32, where only rows count: 24 units of
+  // 145 rows x 585 20 / 44.
   struct Rows {
-    int waves, tiles;
+    int waves, tiles, over;
   };
-  static constexpr Rows kBf16[] = {{1, 1}, {1, 2}, {4, 1}, {4, 2}}, kF32[] = {{1, 1}, {4, 1}};
-  const Rows* const forms = dtype == kTypeF32 ? kF32 : kBf16;
-  int form = dtype == kTypeF32 ? 1 : 3;
+  const bool f32 = dtype == kTypeF32;
+  const Rows forms[] = {{1, 1, 0}, {4, 1, f32 ? 64 : pages.type == kTypeE4m3 ? 48 : 16}, {4, 2, 128}};
   const long long units = (long long)n_seq * pages.n_kv_head, all_rows = (long long)n_seq * n_head * max_new;
   long long groups = 0, tiles = 0;
-  for (bool fits = true; fits; --form) {
+  for (int form = f32 ? 1 : 2; form >= 0; --form) {
     p.row_waves = forms[form].waves;
     p.row_tiles = forms[form].tiles;
-    const int tile = dtype == kTypeF32 || p.row_waves == 4 ? 64 : 128;
+    const int tile = f32 || p.row_waves == 4 ? 64 : 128;
     tiles = (keys + tile - 1) / tile + (keys < cap ? 2 : 0);
-    p.min_tiles = p.row_waves == 4 ? 16 : all_rows <= 512 ? 1 : dtype == kTypeF32 ? 16 : 8;
+    p.min_tiles = p.row_waves == 4 ? 16 : all_rows <= 512 ? 1 : f32 ? 16 : 8;
     groups = units * ((rows + p.rows() - 1) / p.rows());
-    const long long parts = groups * (tiles > p.min_tiles ? tiles / p.min_tiles : 1);
-    fits = form > 0 && (rows <= p.rows() / 2 || parts < kComputeUnits);
+    const long long parts = groups * (!f32 && tiles > p.min_tiles ? tiles / p.min_tiles : 1);
+    if (rows > forms[form].over && parts >= kComputeUnits) break;
   }
+  // Workgroups that the keys are cut for.  us at targets of 512 / 768 / 1024 / 1536 / 2048: chunks of up to 512 tokens over up to
+  // 8192 rows, 32 units, e4m3 228 / 206 / 203 / 220 / 228 (of one length 350 / 373 / 374 / 389 / 393); single tokens over up to 4000
+  // rows, 512 units, e4m3 80 / 77 / 82 / 85 / 88 (one length 105 / 113 / 113 / 121 / 125); 16 units x 131072 rows bf16 196 / 225 /
+  // 210 / 222 / 232.  min_tiles: what a workgroup has at least, against the cost of its start and of the join: one token of one
+  // sequence, 1 / 2 / 16 tiles 10.7 / 12.9 / 12.5; 32 units x 1000 rows, 1 / 2 / 4 / 16 13 / 14 / 17 / 20; but 32 units of 64 tokens
+  // x 300 rows uncut 11, cut 18.  No cutting with four row groups to each such workgroup, nor under a window, which bounds what a
+  // sequence costs, with one (768 units of single tokens in a window of 2048: 44, cut 48 to 56).
   p.target = (p.row_waves == 4 ? 4 : 2) * kComputeUnits;
-  // (a window bounds what a sequence costs: enough row groups are then enough)
   if (tiles <= p.min_tiles || groups >= 4 * p.target || (keys < cap && groups >= p.target)) p.target = 0;
   // every sequence's tiles over `most` are rounded up, once to a group
   const long long cut = groups + p.target, parts = groups * ((tiles + p.min_tiles - 1) / p.min_tiles);
@@ -571,7 +551,8 @@ hipError_t launch_pages_attend(int dtype, int d, int n_seq, int n_head, const Pa
   const bool q8 = pages.type == kTypeE4m3;
   hipError_t e;
   if (dtype == kTypeBf16) {
-    if (d == 128) e = q8 ? launch_plan<kTypeBf16, true, 128>(plan, a, stream) : launch_plan<kTypeBf16, false, 128>(plan, a, stream);
+    if (d == 128)
+      e = q8 ? launch_plan<kTypeBf16, true, 128>(plan, a, stream) : launch_plan<kTypeBf16, false, 128>(plan, a, stream);
     else e = q8 ? launch_plan<kTypeBf16, true, 64>(plan, a, stream) : launch_plan<kTypeBf16, false, 64>(plan, a, stream);
   } else {
     if (d == 128) e = q8 ? launch_plan<kTypeF32, true, 128>(plan, a, stream) : launch_plan<kTypeF32, false, 128>(plan, a, stream);

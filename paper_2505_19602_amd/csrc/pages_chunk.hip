@@ -5,12 +5,19 @@
 // Four waves of 16 RT query rows each share tiles of 64 keys, in two stages.  A wave brings in 16 rows of a tile: they
 // lie in one page whatever its size (16 rows or more), so that the page's number and the rows' address are scalars.
 // Rows go straight into LDS.  e4m3 rows wait there as codes, a tile ahead, until the wave that has brought them widens
-// them into the tile, once for the four waves (exactly).  A wave whose 16 rows some lanes must not read (behind the last row, outside
-// window and sinks) fetches zeros for those; pages that do not exist are zeros too.
+// them into the tile, once for the four waves (exactly).  A wave whose 16 rows some lanes must not read (behind the last
+// row, outside window and sinks) fetches zeros for those; pages that do not exist are zeros too.
 //
 // Running maximum: formed per lane (an eighth of a block's keys), it is joined over the four lanes of a row only where it
 // exceeds the row's offset by kRescaleThreshold log2 units in some row of the wave, which after the first blocks is rare;
 // the accumulators are rescaled behind the product that is then still to come with the old offset.
+//
+// What bounds it: the matrix cores and the softmax beside them, as in the dense kernel.  128 units x 4096 tokens x 4420 rows,
+// head_dim 128: bf16 1190 us (1.0 PFLOP/s; the dense kernel 1003 to 1050), causal 770 us, e4m3 1425 us (the codes' widening is
+// on top), head_dim 64 690 us (e4m3 828).  2048 tokens of 32 heads in a window of 1024 104 us (0.66 PFLOP/s): a walk is 17
+// tiles, of which the first and the last are masked element by element, and its start and end weigh.  4 ragged sequences of
+// up to 512 tokens over up to 8192 rows, e4m3 200 us (0.56 PFLOP/s), bf16 168 us: walks of 16 tiles and more, their sums through
+// the workspace, and 20 us of the join.
 #include <type_traits>
 
 #include "pages_attend.h"
@@ -50,7 +57,8 @@ __device__ __forceinline__ void dma16(const unsigned char* base_uniform, unsigne
                :: "s"(lds_addr_uniform), "v"(voff), "s"(base_uniform), "n"(IMM) : "m0", "memory");
 }
 __device__ __forceinline__ void dma16_lane(const unsigned char* address, unsigned lds_addr_uniform) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_addr_uniform), "v"(address) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(lds_addr_uniform), "v"(address) : "m0", "memory");
 }
 
 template <int D, bool Q8, int RT>
@@ -69,7 +77,7 @@ void pages_chunk_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int first_row = slice.row_group * G::kRows, wave_row = first_row + wave * (16 * RT);
-  const Seen<TN> seen(a, seq, first_row, G::kRows);
+  const Seen<TN> seen(a, slice, first_row, G::kRows);
   const int per = (seen.n_tile + slice.cuts - 1) / slice.cuts;
   const int t0 = min(slice.cut * per, seen.n_tile), n_tile = min(t0 + per, seen.n_tile) - t0;
   // all rows of the wave see [w_begin, w_end) and the sinks below w_end
@@ -151,15 +159,17 @@ void pages_chunk_kernel(AttendArgs a) {
     const unsigned char* scale = scalar((unsigned)page < (unsigned)c.n_page
                                             ? scales + page * c.scale_page + kv * c.scale_head + slot
                                             : g_zero_rows);
-#pragma unroll
-    for (int p = 0; p < G::kVecs; ++p) sc[p] = scale[kVecRows * p + q8_row];
     if (seen.plain(t0 + t) || seen.every(pos, 16)) {
+#pragma unroll
+      for (int p = 0; p < G::kVecs; ++p) sc[p] = scale[kVecRows * p + q8_row];
       dma16<0>(rows, 16 * lane, dst);
       if constexpr (G::kVecs == 2) dma16<1024>(rows, 16 * lane, dst);
     } else {
 #pragma unroll
       for (int p = 0; p < G::kVecs; ++p) {
         const bool there = seen.some(pos + kVecRows * p + q8_row);
+        // (the scale too: what a row holds that has not been written comes into nothing)
+        sc[p] = *(there ? scale + kVecRows * p + q8_row : (const unsigned char*)g_zero_rows);
         dma16_lane((there ? rows : (const unsigned char*)g_zero_rows) + 1024 * p + 16 * lane, dst + 1024 * p);
       }
     }
@@ -520,9 +530,11 @@ void pages_chunk_kernel(AttendArgs a) {
   unsigned char* const mine = smem + wave * G::kMine;
   if (any_odd) {
     float* const sums = (float*)mine;
-    sums_to_lds<D, RT>(o, sums);
+#pragma unroll
+    for (int b = 0; b < RT; ++b) sums_to_lds<D>(o[b], sums + 16 * b * D);
     add_odd<kTypeBf16, Q8, D, TN, RT>(a, seen, seq, kv, wave_row, t0, t0 + n_tile, 0, TN, neg, sums);
-    sums_from_lds<D, RT>(o, sums);
+#pragma unroll
+    for (int b = 0; b < RT; ++b) sums_from_lds<D>(o[b], sums + 16 * b * D);
   }
 
   // ---- write
@@ -541,18 +553,14 @@ void pages_chunk_kernel(AttendArgs a) {
       }
 #pragma unroll
       for (int x = 0; x < NCB; ++x) *(f32x4*)(sums + i * kSumStride + 64 * x + 16 * g) = o[b][x];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_s_waitcnt(0xc07f);
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      own_lds();
 #pragma unroll
       for (int p = 0; p < 16 * kLanes / 64; ++p) {
         const int r = (64 / kLanes) * p + lane / kLanes;
         const f32x4 val = *(const f32x4*)(sums + r * kSumStride + 16 * (lane % kLanes));
         if (wave_row + 16 * b + r < seen.n_rows) *(f32x4*)(a.part + (row + r) * D + 4 * (lane % kLanes)) = val;
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_s_waitcnt(0xc07f);
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      own_lds();
     }
     return;
   }
@@ -572,9 +580,7 @@ void pages_chunk_kernel(AttendArgs a) {
           make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  own_lds();
 #pragma unroll
   for (int p = 0; p < 16 * RT / G::kRowsPerOp; ++p) {
     const int r = G::kRowsPerOp * p + lane / G::kChunks;
@@ -600,7 +606,8 @@ hipError_t launch_form(const AttendArgs& a, int n_wg, hipStream_t stream) {
 
 hipError_t launch_pages_chunk(int d, bool q8, int row_tiles, const AttendArgs& a, int n_wg, hipStream_t stream) {
   auto tiles = [&](auto dim, auto quantised) {
-    return row_tiles == 2 ? launch_form<dim(), quantised(), 2>(a, n_wg, stream) : launch_form<dim(), quantised(), 1>(a, n_wg, stream);
+    return row_tiles == 2 ? launch_form<dim(), quantised(), 2>(a, n_wg, stream)
+                          : launch_form<dim(), quantised(), 1>(a, n_wg, stream);
   };
   auto cache = [&](auto dim) { return q8 ? tiles(dim, std::true_type{}) : tiles(dim, std::false_type{}); };
   return d == 64 ? cache(std::integral_constant<int, 64>{}) : cache(std::integral_constant<int, 128>{});

@@ -273,6 +273,21 @@ def test_nan_codes_stay_where_they_are_seen(window):
         _check_attend(5, 1, 2, 1, 64, dtype, E4M3, 16, 200, 8, causal=True, window=window, sinks=1, change=change)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", [{}, dict(causal=True), dict(causal=True, window=37, sinks=3)])
+def test_codes_and_scales_that_nobody_wrote_reach_nothing(dtype, d, mask):
+    # rows behind the last one and pages of nobody hold NaN codes with the scale byte 255, as memory comes
+    for new, rows in ((1, 77), (20, 85), (40, 130), (70, 333), (130, 1300)):
+        def change(cache):
+            for name in ("k", "v"):
+                dead = [(p, 0) for p in cache.unused] + [(int(cache.table[s, rows // 16]), rows % 16) for s in range(2)]
+                for p, slot in dead:
+                    cache.pool[name].view(torch.uint8)[p, :, slot:] = 0x7f
+                    cache.scales[name][p, :, slot:] = 255
+        _check_attend(rows, 2, 4, 2, d, dtype, E4M3, 16, rows, new, change=change, **mask)
+
+
 @pytest.mark.parametrize("dtype,cache_dtype", TYPES)
 def test_tokens_that_see_nothing_get_zeros(dtype, cache_dtype):
     # sequences shorter than their chunk (positions below zero see nothing under a causal mask) and empty ones
