@@ -134,8 +134,8 @@ void pages_chunk_kernel(AttendArgs a) {
       dma16<0>(rows, ofs(0), dst);
       dma16<1024>(rows, ofs(1), dst);
       if constexpr (G::kOps == 4) {
-        dma16<2048>(rows, ofs(2), dst);
-        dma16<3072>(rows, ofs(3), dst);
+        dma16<2 * 1024>(rows, ofs(2), dst);
+        dma16<3 * 1024>(rows, ofs(3), dst);
       }
     } else {
 #pragma unroll
