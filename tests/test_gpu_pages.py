@@ -34,6 +34,13 @@ def _check_attend(seed, seqs, heads, kv_heads, d, dtype, cache_dtype, page, most
     print(f"attend {seqs} seqs {heads}/{kv_heads} heads d {d} {dtype} cache {cache_dtype} page {page} rows {most} new {new} "
           f"ragged {ragged} packed {packed} causal {causal} window {window} sinks {sinks}", flush=True)
     lens, counts = P.lengths(random.Random(seed), seqs, most, new, ragged)
+    return _check_lengths(seed, lens, counts, heads, kv_heads, d, dtype, cache_dtype, page, new, packed=packed, causal=causal,
+                          window=window, sinks=sinks, scale=scale, width=width, change=change, sm_scale=sm_scale)
+
+
+def _check_lengths(seed, lens, counts, heads, kv_heads, d, dtype, cache_dtype, page, new, *, packed=False, causal=False, window=0,
+                   sinks=0, scale=1.0, width=None, change=None, sm_scale=0.0):
+    seqs = len(lens)
     cache = P.Cache(seed, lens, kv_heads, d, page, cache_dtype, dtype, width=width, scale=scale)
     if change:
         change(cache)
@@ -47,6 +54,8 @@ def _check_attend(seed, seqs, heads, kv_heads, d, dtype, cache_dtype, page, most
     torch.cuda.synchronize()
     got, touched = out.cpu(), torch.zeros(out.shape, dtype=torch.bool)
     for s in range(seqs):
+        if counts[s] == 0:
+            continue
         want, tol = P.attend(cache, s, take(q, s), causal, window, sinks, sm_scale or d ** -0.5)
         have = take(got, s).double()
         same = (have == want) | (have.isnan() & want.isnan())   # infinities and NaN where they belong
@@ -381,3 +390,87 @@ def test_strides_and_orders(dtype, cache_dtype):
         want, tol = P.attend(cache, s, fused[s, :, :heads].transpose(0, 1), True, 0, 0, d ** -0.5)
         assert torch.all((q[s].cpu().double() - want).abs() <= tol)
     assert torch.equal(on[:, :, heads:].cpu(), fused[:, :, heads:])
+
+
+# Workgroups of many query rows are taken where there are many units: 128 sequences, three of them with rows.
+BUSY = (0, 50, 127)
+
+
+def _check_among_many(seed, heads, kv_heads, d, dtype, cache_dtype, rows, new, **kw):
+    print(f"attend among many: {heads}/{kv_heads} heads d {d} {dtype} cache {cache_dtype} rows {rows} new {new} {kw}", flush=True)
+    lens, counts = [0] * 128, [0] * 128
+    for s, n, t in zip(BUSY, (rows, max(rows - 37, 1), rows), (new, max(new // 2, 1), max(new - 1, 1))):
+        lens[s], counts[s] = n, min(n, t)
+    _check_lengths(seed, lens, counts, heads, kv_heads, d, dtype, cache_dtype, 16, new, packed=True, **kw)
+
+
+MASKS = [{}, dict(causal=True), dict(causal=True, window=37, sinks=3), dict(causal=True, window=700, sinks=70)]
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", MASKS)
+def test_attend_many_rows_among_many_sequences(dtype, cache_dtype, d, mask):
+    for new, rows, group in ((17, 65, 1), (65, 66, 1), (49, 64, 1), (33, 190, 2), (130, 333, 1), (129, 129, 1), (200, 1300, 1)):
+        _check_among_many(new, 2 * group, 2, d, dtype, cache_dtype, rows, new, **mask)
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_many_rows_over_cut_keys(dtype, cache_dtype, d):
+    # (keys are cut in pieces of 16 tiles of 64)
+    for new, rows, mask in ((70, 2500, MASKS[1]), (150, 3500, MASKS[0]), (150, 3500, dict(causal=True, window=1900, sinks=5))):
+        _check_among_many(rows, 2, 2, d, dtype, cache_dtype, rows, new, **mask)
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", TYPES)
+def test_attend_many_rows_scores_that_rise_and_fall(dtype, cache_dtype):
+    for where in (0, 31, 32, 64, 150, 299):
+        def change(cache):
+            for s in BUSY:
+                if where < cache.lens[s]:
+                    if cache_dtype == E4M3:
+                        at = (int(cache.table[s, where // 16]), 1, where % 16)
+                        cache.pool["k"][at], cache.scales["k"][at] = torch.full((128,), 384.0).to(E4M3), 120
+                    else:
+                        cache.put("k", s, where, 1, torch.full((128,), 3.0))
+        for new in (80, 150):
+            _check_among_many(where, 2, 2, 128, dtype, cache_dtype, 300, new, scale=2.0, change=change)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("window", [0, 5, 40])
+def test_many_rows_what_a_token_does_not_see_does_not_reach_it(dtype, d, value, window):
+    for new, rows in ((70, 70), (70, 150), (150, 200), (70, 2500), (150, 2500)):
+        def change(cache):
+            for s in BUSY:
+                n = cache.lens[s]
+                for r in {0, 3, n - new // 2, n - 1, n - 2, max(0, n - 45)}:
+                    if 0 <= r < n:
+                        cache.pool["v"][int(cache.table[s, r // 16]), 0, r % 16, 3::7] = value
+                cache.pool["k"][int(cache.table[s, (n - 1) // 16]), 1, (n - 1) % 16, 0] = math.nan
+                for name in ("k", "v"):
+                    cache.pool[name][cache.unused] = math.nan
+                    if n % 16:
+                        cache.pool[name][int(cache.table[s, n // 16]), :, n % 16:] = math.nan
+        _check_among_many(rows, 2, 2, d, dtype, dtype, rows, new, causal=True, window=window, sinks=2, change=change)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", MASKS)
+def test_many_rows_codes_and_scales_that_nobody_wrote(dtype, d, mask):
+    for new, rows in ((70, 77), (130, 333), (150, 2500)):
+        def change(cache):
+            for name in ("k", "v"):
+                for s in BUSY:
+                    n = cache.lens[s]
+                    dead = [(p, 0) for p in cache.unused] + ([(int(cache.table[s, n // 16]), n % 16)] if n % 16 else [])
+                    for p, slot in dead:
+                        cache.pool[name].view(torch.uint8)[p, :, slot:] = 0x7f
+                        cache.scales[name][p, :, slot:] = 255
+                    for r in (0, 2, n - 30):     # and NaN codes in rows that are seen
+                        cache.pool["v"].view(torch.uint8)[int(cache.table[s, r // 16]), 1, r % 16, 1::5] = 0x7f
+        _check_among_many(rows, 2, 2, d, dtype, E4M3, rows, new, change=change, **mask)
