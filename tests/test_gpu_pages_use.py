@@ -280,7 +280,10 @@ def _run_all():
             (2, 3, 3, 64, BF16, E4M3, 16, 700, 300, dict()),
             (2, 16, 16, 128, BF16, BF16, 64, 4000, 130, dict(causal=True)),
             (2, 2, 2, 128, F32, F32, 16, 3000, 3, dict(causal=True)),
-            (2, 2, 2, 64, F32, E4M3, 16, 300, 70, dict(causal=True, window=64)))):
+            (2, 2, 2, 64, F32, E4M3, 16, 300, 70, dict(causal=True, window=64)),
+            (130, 2, 2, 64, BF16, E4M3, 16, 1300, 70, dict(causal=True)),
+            (130, 2, 2, 128, BF16, BF16, 64, 1300, 150, dict()),
+            (130, 2, 2, 64, F32, F32, 16, 1300, 80, dict(causal=True)))):
         print(f"workgroup order: pages {S}x{H}/{kv} d {d} {dtype} {cache_dtype} rows {most} new {new} {mask}", flush=True)
         lens, counts = P.lengths(random.Random(n), S, most, new, True)
         pages = P.Cache(n, lens, kv, d, page, cache_dtype, dtype).on(DEV)
