@@ -373,8 +373,8 @@ typedef struct {
 
 /* Writes k_new / v_new [n_kv_head heads] of the new tokens into their pages: quantised if the cache is
  * SCALEKV_E4M3, else bit for bit.  No other row of the pool is touched.  Sequences that write must not share the
- * pages written.  k_new / v_new must not overlap the pool, nor k and v (or the scales) each other:
- * INVALID_ARG. */
+ * pages written.  k_new / v_new must not overlap the pool, nor k and v (or the scales) each other, and where
+ * chunk->first is given both must have the same n_row: INVALID_ARG. */
 scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pages* pages,
                                    const scalekv_rows* k_new, const scalekv_rows* v_new,
                                    const scalekv_chunk* chunk, void* stream);
@@ -401,7 +401,8 @@ scalekv_status scalekv_pages_workspace_bytes(const scalekv_shape* shape, const s
  * The key axis is split over workgroups where few rows meet long caches; sums are joined in a fixed order, results are
  * reproducible bit for bit.  The workspace holds nothing between calls; calls that may overlap in time need
  * one each.  out may lie exactly on q (same pointer and strides); any other overlap of `out` with q, the pool or
- * ws, and rows of `out` that coincide (a stride of 0) -> INVALID_ARG. */
+ * ws, rows of `out` that coincide (a stride of 0), and another n_row of `out` than of q where chunk->first is
+ * given -> INVALID_ARG. */
 scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pages* pages,
                                     const scalekv_rows* q, const scalekv_chunk* chunk,
                                     const scalekv_mask* mask, const scalekv_rows* out, void* ws,

@@ -96,6 +96,16 @@ scalekv_status check_token_rows(const scalekv_shape* s, const scalekv_rows* r, c
   return SCALEKV_OK;
 }
 
+// Two tensors of token rows: where `first` places the tokens, row first[s] + t of both belongs to the same token, and what
+// lies behind the end of the shorter one would be left out without a word.  (Otherwise max_new rows of each are looked at.)
+scalekv_status check_same_rows(const scalekv_rows* a, const char* name_a, const scalekv_rows* b, const char* name_b,
+                               const scalekv_chunk* chunk) {
+  if (chunk->first && a->n_row != b->n_row)
+    return fail(SCALEKV_ERR_INVALID_ARG, "%s has %d rows and %s %d: they must have the same number where first is given",
+                name_a, a->n_row, name_b, b->n_row);
+  return SCALEKV_OK;
+}
+
 struct Span {
   uintptr_t lo, hi;
 };
@@ -200,6 +210,7 @@ scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pag
   SCALEKV_TRY(check_chunk(shape, chunk));
   SCALEKV_TRY(check_token_rows(shape, k_new, chunk, "k_new"));
   SCALEKV_TRY(check_token_rows(shape, v_new, chunk, "v_new"));
+  SCALEKV_TRY(check_same_rows(k_new, "k_new", v_new, "v_new", chunk));
   if (meets_pool(shape, pages, rows_span(shape, k_new, pages->n_kv_head)) ||
       meets_pool(shape, pages, rows_span(shape, v_new, pages->n_kv_head)))
     return fail(SCALEKV_ERR_INVALID_ARG, "k_new or v_new overlaps the pool");
@@ -268,6 +279,7 @@ scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pa
   SCALEKV_TRY(check_chunk(shape, chunk));
   SCALEKV_TRY(check_token_rows(shape, q, chunk, "q"));
   SCALEKV_TRY(check_token_rows(shape, out, chunk, "out"));
+  SCALEKV_TRY(check_same_rows(q, "q", out, "out", chunk));
   MaskView m;
   SCALEKV_TRY(check_mask(mask, &m));
   if (out->n_row == 0) return SCALEKV_OK;

@@ -237,6 +237,21 @@ def test_the_binding_refuses_tensors_that_are_not_what_it_says():
             skv.Pages(*args)
 
 
+def test_packed_tensors_of_different_lengths_are_refused(L):
+    # a sequence's tokens lie at the same rows of both: behind the end of the shorter one they would be left out, unsaid
+    chunk = _chunk(first=0x7000000, count=0x7100000)
+    rows = lambda n, at=0x5000000: _rows(ptr=at if n else 0, seq_stride=0, n_row=n)
+    for a, b in ((8, 5), (5, 8), (8, 0), (0, 8), (1, 2)):
+        assert _write(L, k=rows(a), v=rows(b, 0x6000000), chunk=chunk) == INVALID, (a, b)
+        assert f"k_new has {a} rows and v_new {b}" in _err(L)
+        assert _attend(L, q=rows(a), out=rows(b, 0x6000000), chunk=chunk) == INVALID, (a, b)
+        assert f"q has {a} rows and out {b}" in _err(L)
+    # rows of a sequence that lie behind max_new are not looked at: dense tensors may have more of them
+    inside = 0x2000000                                                # (refused behind that check, before a launch)
+    assert _attend(L, q=_rows(n_row=9), out=_rows(ptr=inside)) == INVALID and "overlaps the pool" in _err(L)
+    assert _write(L, k=_rows(n_row=9), v=_rows(ptr=inside)) == INVALID and "overlaps the pool" in _err(L)
+
+
 # ---- the definitions in 64 bits that the GPU tests use
 
 def test_codes_are_the_nearest_e4m3_values_ties_to_even():
