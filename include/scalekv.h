@@ -402,7 +402,8 @@ scalekv_status scalekv_pages_workspace_bytes(const scalekv_shape* shape, const s
  * reproducible bit for bit.  The workspace holds nothing between calls; calls that may overlap in time need
  * one each.  out may lie exactly on q (same pointer and strides); any other overlap of `out` with q, the pool or
  * ws, rows of `out` that coincide (a stride of 0), and another n_row of `out` than of q where chunk->first is
- * given -> INVALID_ARG. */
+ * given -> INVALID_ARG.  A row of packed tensors belongs to one sequence: `first` and `count` are device memory, host
+ * copies are checked by scalekv_pages_check_packed. */
 scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pages* pages,
                                     const scalekv_rows* q, const scalekv_chunk* chunk,
                                     const scalekv_mask* mask, const scalekv_rows* out, void* ws,
@@ -418,6 +419,14 @@ scalekv_status scalekv_pages_check(const scalekv_shape* shape, const scalekv_pag
                                    const int32_t* table, const int32_t* len,
                                    const scalekv_chunk* chunk, const int32_t* first,
                                    const int32_t* count, int32_t n_row);
+
+/* Host only: checks where the new tokens of packed tensors lie (one tensor for all sequences, seq_stride 0), from host copies
+ * of first and count [n_seq] (count NULL as in `chunk`, whose own pointers are not read); n_row: of those tensors.
+ * INVALID_ARG, and a message that names the sequences, for: a count outside [0, max_new]; rows outside [0, n_row); a row that
+ * two sequences share: attention would leave the result of either in it.  (scalekv_pages_check does not know whether
+ * tensors are packed: in a padded batch rows are counted anew in each sequence.) */
+scalekv_status scalekv_pages_check_packed(const scalekv_shape* shape, const scalekv_chunk* chunk,
+                                          const int32_t* first, const int32_t* count, int32_t n_row);
 
 /* Benchmark aid, not part of the method.  events: host array of 5 hipEvent_t
  * (created by the caller with timing enabled), or NULL to switch off.  While

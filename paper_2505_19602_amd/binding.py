@@ -36,7 +36,7 @@ _STATUS_SYMBOLS = (
     "scalekv_window_centroids", "scalekv_select_window", "scalekv_step_append_first",
     "scalekv_asi", "scalekv_drafter_set", "scalekv_allocate_budgets", "scalekv_select_positional",
     "scalekv_pyramid_budgets", "scalekv_policy_table", "scalekv_pages_write", "scalekv_pages_read",
-    "scalekv_pages_workspace_bytes", "scalekv_pages_attend", "scalekv_pages_check",
+    "scalekv_pages_workspace_bytes", "scalekv_pages_attend", "scalekv_pages_check", "scalekv_pages_check_packed",
 )
 EXPORTED_SYMBOLS = _STATUS_SYMBOLS + ("scalekv_last_error", "scalekv_version")
 
@@ -769,13 +769,19 @@ def pages_attend(shape: Shape, pages: Pages, q: torch.Tensor, out: torch.Tensor,
 
 def pages_check(shape: Shape, pages: Pages, table: Sequence[Sequence[int]], lens: Sequence[int],
                 first: Optional[Sequence[int]] = None, count: Optional[Sequence[int]] = None,
-                max_new: Optional[int] = None, n_row: int = 0) -> None:
+                max_new: Optional[int] = None, n_row: int = 0, packed: bool = False) -> None:
     """scalekv_pages_check: host copies of the table, the lengths and (with max_new) what is new, against the sizes of
-    `pages`; n_row: token rows of a sequence (packed: of all).  Raises what the kernels would skip or read as zeros."""
+    `pages`; n_row: token rows of a sequence (packed: of all).  Raises what the kernels would skip or read as zeros.
+    packed: the tokens lie in tensors [N, H, d], no row of which may belong to two sequences (scalekv_pages_check_packed)."""
     cs, width = shape.c(), pages.table.shape[1]
-    if len(table) != shape.n_seq or any(len(r) != width for r in table) or len(lens) != shape.n_seq or             any(x is not None and len(x) != shape.n_seq for x in (first, count)):
+    if len(table) != shape.n_seq or any(len(r) != width for r in table) or len(lens) != shape.n_seq or \
+            any(x is not None and len(x) != shape.n_seq for x in (first, count)):
         raise ScaleKVError(1, f"expected table [{shape.n_seq}][{width}] and {shape.n_seq} lengths, firsts and counts")
+    if packed and (first is None or max_new is None):
+        raise ScaleKVError(1, "first and max_new are needed where tensors are packed")
     ints = lambda x: None if x is None else (ctypes.c_int32 * len(x))(*[index(i) for i in x])
     chunk = None if max_new is None else ctypes.byref(_CChunk(index(max_new), 0, 0))
     _check(lib().scalekv_pages_check(ctypes.byref(cs), ctypes.byref(pages.c), ints([i for r in table for i in r]), ints(lens),
                                      chunk, ints(first), ints(count), index(n_row)))
+    if packed:
+        _check(lib().scalekv_pages_check_packed(ctypes.byref(cs), chunk, ints(first), ints(count), index(n_row)))

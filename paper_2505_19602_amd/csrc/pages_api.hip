@@ -1,5 +1,7 @@
 // C ABI of the paged cache: argument checks and launches.
 #include <algorithm>
+#include <new>
+#include <vector>
 
 #include "api_checks.h"
 #include "pages.h"
@@ -349,6 +351,38 @@ scalekv_status scalekv_pages_check(const scalekv_shape* shape, const scalekv_pag
             return fail(SCALEKV_ERR_INVALID_ARG, "page %d receives new tokens of sequence %d and is table[%d][%d] too", page,
                         s, o, j);
     }
+  }
+  return SCALEKV_OK;
+}
+
+scalekv_status scalekv_pages_check_packed(const scalekv_shape* shape, const scalekv_chunk* chunk, const int32_t* first,
+                                          const int32_t* count, int32_t n_row) {
+  SCALEKV_TRY(check_shape(shape));
+  SCALEKV_TRY(check_chunk(shape, chunk));
+  if (!first) return fail(SCALEKV_ERR_INVALID_ARG, "first is NULL");
+  auto new_of = [&](int s) { return count ? count[s] : chunk->max_new; };
+  // the sequence whose tokens begin at each row: where ranges meet, two neighbours among them do
+  std::vector<int> by_row;
+  try {
+    for (int s = 0; s < shape->n_seq; ++s) {
+      const int n = new_of(s);
+      if (n < 0 || n > chunk->max_new)
+        return fail(SCALEKV_ERR_INVALID_ARG, "count[%d] = %d is outside 0..%d", s, n, chunk->max_new);
+      if (n == 0) continue;
+      const long long at = first[s];
+      if (at < 0 || at + n > n_row)
+        return fail(SCALEKV_ERR_INVALID_ARG, "rows %lld..%lld of sequence %d are outside 0..%d", at, at + n - 1, s, n_row - 1);
+      by_row.push_back(s);
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(SCALEKV_ERR_INVALID_ARG, "no memory for %d sequences", shape->n_seq);
+  }
+  std::sort(by_row.begin(), by_row.end(),
+            [&](int a, int b) { return first[a] != first[b] ? first[a] < first[b] : a < b; });
+  for (size_t i = 1; i < by_row.size(); ++i) {
+    const int a = by_row[i - 1], b = by_row[i];
+    if (first[b] < first[a] + new_of(a))
+      return fail(SCALEKV_ERR_INVALID_ARG, "sequences %d and %d share row %d", std::min(a, b), std::max(a, b), first[b]);
   }
   return SCALEKV_OK;
 }

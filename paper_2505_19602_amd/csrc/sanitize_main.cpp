@@ -148,6 +148,12 @@ int main() {
     EXPECT(scalekv_pages_write(&s, &far, &rows, &rows, &chunk, nullptr) == SCALEKV_ERR_INVALID_ARG);
     std::vector<int32_t> table{4, 5, 6}, len{90}, count{8}, first{0};
     EXPECT(scalekv_pages_check(&s, &pg, table.data(), len.data(), &chunk, first.data(), count.data(), 8) == SCALEKV_OK);
+    scalekv_shape two = s;
+    two.n_seq = 2;
+    std::vector<int32_t> firsts{3, 0}, counts{5, 4};
+    EXPECT(scalekv_pages_check_packed(&two, &chunk, firsts.data(), counts.data(), 8) == SCALEKV_ERR_INVALID_ARG);
+    counts[1] = 3;
+    EXPECT(scalekv_pages_check_packed(&two, &chunk, firsts.data(), counts.data(), 8) == SCALEKV_OK);
     count[0] = 9;
     EXPECT(scalekv_pages_check(&s, &pg, table.data(), len.data(), &chunk, first.data(), count.data(), 8) == SCALEKV_ERR_INVALID_ARG);
     table[2] = 10;

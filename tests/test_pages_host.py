@@ -252,6 +252,42 @@ def test_packed_tensors_of_different_lengths_are_refused(L):
     assert _write(L, k=_rows(n_row=9), v=_rows(ptr=inside)) == INVALID and "overlaps the pool" in _err(L)
 
 
+def test_packed_rows_that_two_sequences_share_are_named(L):
+    def check(first, count, max_new=8, n_row=30):
+        ints = lambda x: None if x is None else (ctypes.c_int32 * len(x))(*x)
+        return L.scalekv_pages_check_packed(ctypes.byref(_shape(n_seq=len(first), n_head=1)),
+                                            ctypes.byref(_chunk(max_new=max_new)), ints(first), ints(count), n_row)
+    for first, count in (([0, 8], None), ([8, 0], None), ([0, 3, 5], [3, 2, 8]), ([5, 0, 3], [8, 3, 2]), ([22, 0], [8, 8]),
+                         ([4, 4, 4], [0, 5, 0]), ([0, -9, 99], [8, 0, 0]), ([0, 5, 3], [5, 8, 0])):
+        assert check(first, count) == OK, (first, count, _err(L))
+    for first, count, word in (([0, 7], None, "sequences 0 and 1"), ([3, 0, 5], [3, 2, 8], "sequences 0 and 2"),
+                               ([4, 4], [1, 1], "sequences 0 and 1"), ([0, 20, 2], [8, 1, 1], "sequences 0 and 2"),
+                               ([0, 2, 20], [8, 1, 1], "sequences 0 and 1"), ([0, 23], None, "rows 23..30 of sequence 1"),
+                               ([0, -1], [8, 1], "sequence 1"), ([0, 8], [8, 9], "count[1]"), ([0, 8], [-1, 8], "count[0]"),
+                               ([0, 2 ** 31 - 1], [1, 8], "sequence 1")):
+        assert check(first, count) == INVALID and word in _err(L), (first, count, _err(L))
+    assert check([0, 0], None, max_new=0) == INVALID and "max_new" in _err(L)
+    one = _shape()
+    assert L.scalekv_pages_check_packed(ctypes.byref(one), ctypes.byref(_chunk()), None, None, 8) == INVALID
+    assert "first is NULL" in _err(L)
+    assert L.scalekv_pages_check_packed(ctypes.byref(one), None, None, None, 8) == INVALID and "chunk is NULL" in _err(L)
+    assert L.scalekv_pages_check_packed(None, None, None, None, 8) == INVALID
+
+
+def test_the_binding_checks_packed_rows_where_it_is_told_to():
+    class Sizes:                                                      # (pages without a device: sizes alone are looked at)
+        table, c = torch.zeros(2, 3, dtype=torch.int32), _pages(table_width=3)
+    shape, table = skv.Shape(2, 4, 128, torch.bfloat16), [[0, 1, 2], [3, 4, 5]]
+    call = lambda first, **kw: skv.pages_check(shape, Sizes, table, [40, 90], first=first, max_new=4, n_row=8, **kw)
+    call([4, 0], packed=True)
+    call([0, 3])                                                      # a padded batch: its rows are those of each sequence
+    with pytest.raises(skv.ScaleKVError, match="sequences 0 and 1"):
+        call([0, 3], packed=True)
+    for kw in (dict(first=None, max_new=4), dict(first=[0, 4])):
+        with pytest.raises(skv.ScaleKVError, match="packed"):
+            skv.pages_check(shape, Sizes, table, [40, 90], n_row=8, packed=True, **kw)
+
+
 # ---- the definitions in 64 bits that the GPU tests use
 
 def test_codes_are_the_nearest_e4m3_values_ties_to_even():
