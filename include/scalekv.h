@@ -401,7 +401,7 @@ scalekv_status scalekv_pages_workspace_bytes(const scalekv_shape* shape, const s
  * The key axis is split over workgroups where few rows meet long caches; sums are joined in a fixed order, results are
  * reproducible bit for bit.  The workspace holds nothing between calls; calls that may overlap in time need
  * one each.  out may lie exactly on q (same pointer and strides); any other overlap of `out` with q, the pool or
- * ws, rows of `out` that coincide (a stride of 0), and another n_row of `out` than of q where chunk->first is
+ * ws, rows of `out` that share bytes with each other, and another n_row of `out` than of q where chunk->first is
  * given -> INVALID_ARG.  A row of packed tensors belongs to one sequence: `first` and `count` are device memory, host
  * copies are checked by scalekv_pages_check_packed. */
 scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pages* pages,

@@ -158,6 +158,36 @@ bool pools_meet(const void* a, const void* b, long long n_page, long long page, 
   return false;
 }
 
+// Do two of the rows at i * stride[0] + j * stride[1] + k * stride[2], i < n[0] and so on, share bytes?  Rows of d elements,
+// which each stride between several rows holds.
+bool rows_coincide(const long long (&n)[3], const long long (&stride)[3], int d) {
+  int by[3] = {0, 1, 2};
+  std::sort(by, by + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+  long long reach = d;  // of the dimensions before
+  bool nested = true;
+  for (const int x : by) {
+    if (n[x] == 1) continue;
+    nested = nested && stride[x] >= reach;
+    reach += (n[x] - 1) * stride[x];
+  }
+  if (nested) return false;
+  // Differences of two rows: of the two dimensions with the fewest rows all (the first not negative: a pair has two signs),
+  // and of the third the two that bring them nearest to zero.
+  std::sort(by, by + 3, [&](int a, int b) { return n[a] < n[b]; });
+  const int x = by[0], y = by[1], z = by[2];
+  for (long long i = 0; i < n[x]; ++i)
+    for (long long j = 1 - n[y]; j < n[y]; ++j) {
+      const long long at = i * stride[x] + j * stride[y];
+      const long long k0 = (at < 0 ? -at : at) / stride[z];  // k: less k0, or less k0 + 1, towards zero
+      for (long long k = k0; k <= k0 + 1; ++k) {
+        if (k >= n[z] || (i == 0 && j == 0 && k == 0)) continue;
+        const long long apart = (at < 0 ? -at : at) - k * stride[z];
+        if (apart < d && -apart < d) return true;
+      }
+    }
+  return false;
+}
+
 PagesView pages_view(const scalekv_shape* s, const scalekv_pages* c) {
   PagesView v;
   const long long e = cache_elem_bytes(c);
@@ -285,14 +315,21 @@ scalekv_status scalekv_pages_attend(const scalekv_shape* shape, const scalekv_pa
   MaskView m;
   SCALEKV_TRY(check_mask(mask, &m));
   if (out->n_row == 0) return SCALEKV_OK;
-  if ((shape->n_head > 1 && out->head_stride < shape->head_dim) || (out->n_row > 1 && out->row_stride < shape->head_dim) ||
-      (shape->n_seq > 1 && !chunk->first && out->seq_stride < shape->head_dim))
-    return fail(SCALEKV_ERR_INVALID_ARG, "rows of out coincide: a stride is below head_dim");
+  // (packed: no stride between sequences, whose rows are those of one tensor)
+  const bool packed = chunk->first && out->seq_stride == 0;
+  const long long n[3] = {packed ? 1 : shape->n_seq, shape->n_head, chunk->first ? out->n_row : chunk->max_new};
+  const long long strides[3] = {out->seq_stride, out->head_stride, out->row_stride};
+  for (int x = 0; x < 3; ++x)
+    if (n[x] > 1 && strides[x] < shape->head_dim)
+      return fail(SCALEKV_ERR_INVALID_ARG, "rows of out coincide: a stride is below head_dim");
   const Span o = rows_span(shape, out, shape->n_head);
   const bool on_q = out->ptr == q->ptr && out->seq_stride == q->seq_stride && out->head_stride == q->head_stride &&
                     out->row_stride == q->row_stride;
   if (!on_q && meet(o, rows_span(shape, q, shape->n_head)))
     return fail(SCALEKV_ERR_INVALID_ARG, "out overlaps q and does not lie exactly on it");
+  if (rows_coincide(n, strides, shape->head_dim))
+    return fail(SCALEKV_ERR_INVALID_ARG, "rows of out coincide: strides %lld, %lld and %lld for %lld x %lld x %lld rows of %d",
+                strides[0], strides[1], strides[2], n[0], n[1], n[2], shape->head_dim);
   if (meets_pool(shape, pages, o)) return fail(SCALEKV_ERR_INVALID_ARG, "out overlaps the pool");
   PagesPlan plan;
   SCALEKV_TRY(make_plan(shape, pages, chunk->max_new, m, &plan));

@@ -2,8 +2,10 @@
 dereferenced: every call is refused before a launch), the host check of tables, and the 64-bit definitions that the GPU
 tests compare with.  No GPU needed."""
 import ctypes
+import itertools
 import math
 import os
+import random
 
 import numpy as np
 import pytest
@@ -286,6 +288,39 @@ def test_the_binding_checks_packed_rows_where_it_is_told_to():
     for kw in (dict(first=None, max_new=4), dict(first=[0, 4])):
         with pytest.raises(skv.ScaleKVError, match="packed"):
             skv.pages_check(shape, Sizes, table, [40, 90], n_row=8, packed=True, **kw)
+
+
+def test_rows_of_out_that_coincide_are_refused_whatever_the_strides(L):
+    # every stride holds a row, and yet two rows share bytes; the calls that pass come to the check against the pool, and end there
+    d = 128
+
+    def verdict(seqs, heads, rows, seq, head, row, n_row=0, **more):
+        out = _rows(ptr=0x1000000, seq_stride=seq, head_stride=head, row_stride=row, n_row=n_row or rows)
+        q = _rows(ptr=0x40000000, n_row=n_row or rows)
+        st = _attend(L, _shape(n_seq=seqs, n_head=heads), q=q, out=out, chunk=_chunk(max_new=rows, **more))
+        assert st == INVALID and ("coincide" in _err(L)) != ("overlaps the pool" in _err(L)), (st, _err(L))
+        return "coincide" in _err(L)
+
+    assert verdict(1, 4, 8, 0, d, d) and verdict(1, 4, 8, 0, 7 * d, d) and verdict(1, 4, 8, 0, d, 3 * d)
+    assert verdict(2, 4, 8, 8 * d, 8 * d, d) and verdict(2, 2, 1, d, d, 0) and verdict(2, 2, 8, 8 * d, 16 * d, d + 8)
+    assert not verdict(1, 4, 8, 0, d, 4 * d) and not verdict(1, 4, 8, 0, 8 * d, d) and not verdict(2, 2, 1, d, 2 * d, 0)
+    assert not verdict(1, 2, 4, 0, 3 * d, 2 * d)                      # (no dimension holds another whole: rows 0 2 4 6, 3 5 7 9)
+    assert verdict(1, 4, 4, 0, 3 * d, 2 * d)
+    assert not verdict(2, 4, 4, 4 * d, 8 * d, d, n_row=8)             # (rows behind max_new are not written)
+    assert verdict(2, 4, 4, 4 * d, 8 * d, d, n_row=8, first=0x7000000)   # (but where first places the tokens they may be)
+    assert not verdict(2, 4, 4, 0, d, 4 * d, n_row=8, first=0x7000000)   # packed
+    rng = random.Random(1)
+    found = [0, 0]
+    for _ in range(3000):
+        n = [rng.choice((1, 2, 2, 4, 6)), rng.choice((2, 4, 6)), rng.randint(1, 5)]
+        strides = [d + 8 * rng.randint(0, rng.choice((3, 40, 120))) for _ in range(3)]
+        starts = sorted(sum(x * y for x, y in zip(at, strides)) for at in itertools.product(*map(range, n)))
+        want = any(b - a < d for a, b in zip(starts, starts[1:]))
+        assert verdict(*n, *strides) == want, (n, strides)
+        found[want] += 1
+    assert min(found) > 100
+    # many rows, in dimensions that lie in each other
+    assert not verdict(1024, 2, 8, 8 * 8 * d, 8 * d, d) and verdict(1024, 2, 8, 2 * 8 * d, 8 * d - 8, d)
 
 
 # ---- the definitions in 64 bits that the GPU tests use
