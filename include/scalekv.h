@@ -374,7 +374,8 @@ typedef struct {
 /* Writes k_new / v_new [n_kv_head heads] of the new tokens into their pages: quantised if the cache is
  * SCALEKV_E4M3, else bit for bit.  No other row of the pool is touched.  Sequences that write must not share the
  * pages written.  k_new / v_new must not overlap the pool, nor k and v (or the scales) each other, and where
- * chunk->first is given both must have the same n_row: INVALID_ARG. */
+ * chunk->first is given both must have the same n_row: INVALID_ARG.  k, v and the scales of a page may lie in one record
+ * (the page strides, in bytes, are the record's then; scales of another page stride have to lie outside the pool). */
 scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pages* pages,
                                    const scalekv_rows* k_new, const scalekv_rows* v_new,
                                    const scalekv_chunk* chunk, void* stream);

@@ -158,6 +158,23 @@ bool pools_meet(const void* a, const void* b, long long n_page, long long page, 
   return false;
 }
 
+// Does a pool share bytes with scales whose pages lie as far apart as its own (in one record, say)?  Codes lie at i * page +
+// h * head, `unit` bytes each, scales `gap` bytes on at i * page + h * scale_head, `rows` bytes each.
+bool record_meets(long long gap, long long n_page, long long page, int n_head, long long head, long long unit,
+                  long long scale_head, long long rows) {
+  auto floor_div = [](long long a, long long b) { return a / b - (a % b < 0); };
+  for (int g = 0; g < n_head; ++g) {
+    const long long at = gap + g * scale_head, first = floor_div(at, page);
+    for (long long i = first; i <= first + 1; ++i) {  // the codes' page, counted from the scales'
+      if (i <= -n_page || i >= n_page) continue;
+      const long long x = at - i * page, below = floor_div(x, head);
+      for (long long h = below; h <= below + 1; ++h)
+        if (h >= 0 && h < n_head && h * head < x + rows && x < h * head + unit) return true;
+    }
+  }
+  return false;
+}
+
 // Do two of the rows at i * stride[0] + j * stride[1] + k * stride[2], i < n[0] and so on, share bytes?  Rows of d elements,
 // which each stride between several rows holds.
 bool rows_coincide(const long long (&n)[3], const long long (&stride)[3], int d) {
@@ -255,7 +272,10 @@ scalekv_status scalekv_pages_write(const scalekv_shape* shape, const scalekv_pag
       return fail(SCALEKV_ERR_INVALID_ARG, "pages.k_scale and pages.v_scale overlap");
     for (const void* p : {pages->k, pages->v})
       for (const void* q : {pages->k_scale, pages->v_scale})
-        if (meet(pool_span(shape, pages, p), scale_span(pages, q)))
+        if (meet(pool_span(shape, pages, p), scale_span(pages, q)) &&
+            (pages->scale_page_stride != pages->page_stride ||
+             record_meets(static_cast<const char*>(q) - static_cast<const char*>(p), pages->n_page, pages->page_stride,
+                          pages->n_kv_head, pages->head_stride, unit, pages->scale_head_stride, pages->page_rows)))
           return fail(SCALEKV_ERR_INVALID_ARG, "the scales overlap the pool");
   }
   if (k_new->n_row == 0 && v_new->n_row == 0) return SCALEKV_OK;

@@ -323,6 +323,48 @@ def test_rows_of_out_that_coincide_are_refused_whatever_the_strides(L):
     assert not verdict(1024, 2, 8, 8 * 8 * d, 8 * d, d) and verdict(1024, 2, 8, 2 * 8 * d, 8 * d - 8, d)
 
 
+def test_scales_may_lie_beside_the_codes_of_their_page(L):
+    # packed tensors without rows: an accepted call ends before a launch
+    none, chunk = _rows(ptr=0, n_row=0, seq_stride=0), _chunk(first=0x7000000, count=0x7100000)
+
+    def verdict(at, page, head, scale_head, n_page=10, scale_page=None, heads=2):
+        pages = _pages(dtype=E4M3, v=0x9000000, page_stride=page, head_stride=head, n_page=n_page, n_kv_head=heads,
+                       scale_page_stride=scale_page or page, scale_head_stride=scale_head, k_scale=0x1000000 + at,
+                       v_scale=0xa000000)
+        st = _write(L, _shape(n_head=heads), pages, none, none, chunk)
+        assert st == OK or (st == INVALID and "scales overlap the pool" in _err(L)), (st, _err(L))
+        return st == OK
+
+    unit = 32 * 128                                                   # codes of a head: 4096 bytes, scales: 32
+    record = 2 * (2 * unit + 64)
+    assert verdict(2 * unit, record, unit, 32) and verdict(2 * unit + 64, record, unit, 32)
+    assert verdict(unit, record, unit + 32, unit + 32)                # head by head: codes, scales
+    assert verdict(-64, record, unit, 32) and verdict(2 * unit - record, record, unit, 32)
+    assert not verdict(2 * unit - 1, record, unit, 32) and not verdict(record - 63, record, unit, 32)
+    assert not verdict(unit - 1, record, unit + 32, unit + 32) and not verdict(unit + 1, record, unit + 32, unit + 32)
+    assert not verdict(2 * unit, record, unit, 32, scale_page=record + 16)   # pages' strides that differ: refused within the span
+    assert verdict(10 * record, record, unit, 32) and not verdict(10 * record, record, unit, 32, n_page=11, scale_page=64)
+    # keys and values with their scales in one record
+    pages = _pages(dtype=E4M3, v=0x1000000 + 2 * unit, page_stride=2 * 2 * unit + 128, k_scale=0x1000000 + 4 * unit,
+                   v_scale=0x1000000 + 4 * unit + 64, scale_page_stride=2 * 2 * unit + 128)
+    assert _write(L, pages=pages, k=none, v=none, chunk=chunk) == OK
+    rng, found = random.Random(2), [0, 0]
+    for _ in range(3000):
+        heads, n_page = rng.choice((1, 2, 4)), rng.randint(1, 4)
+        head, scale_head = unit + 16 * rng.randint(0, 9), rng.choice((32, 40, unit, unit + 16 * rng.randint(0, 9)))
+        page = max(heads * head, heads * scale_head) + 16 * rng.randint(0, 30)
+        if rng.random() < 0.5:                                        # around a head's or a page's end
+            at = rng.randint(-n_page, n_page) * page + rng.randint(0, heads) * head + rng.randint(-40, 200)
+        else:
+            at = rng.randint(-n_page * page - 9, n_page * page + 9)
+        codes = [(i * page + h * head, i * page + h * head + unit) for i in range(n_page) for h in range(heads)]
+        scales = [(at + i * page + h * scale_head, at + i * page + h * scale_head + 32) for i in range(n_page) for h in range(heads)]
+        want = not any(a < y and x < b for a, b in codes for x, y in scales)
+        assert verdict(at, page, head, scale_head, n_page, heads=heads) == want, (at, page, head, scale_head, n_page, heads)
+        found[want] += 1
+    assert min(found) > 300, found
+
+
 # ---- the definitions in 64 bits that the GPU tests use
 
 def test_codes_are_the_nearest_e4m3_values_ties_to_even():
