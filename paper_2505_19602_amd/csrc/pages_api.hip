@@ -74,8 +74,8 @@ scalekv_status check_chunk(const scalekv_shape* s, const scalekv_chunk* chunk) {
   if (!chunk) return fail(SCALEKV_ERR_INVALID_ARG, "chunk is NULL");
   if (chunk->max_new < 1) return fail(SCALEKV_ERR_INVALID_ARG, "chunk.max_new must be >= 1 (got %d)", chunk->max_new);
   SCALEKV_TRY(check_rows(s, chunk->max_new, "chunk.max_new"));
-  // rows are numbered over all sequences and heads, in int32
-  if ((long long)s->n_seq * s->n_head * chunk->max_new > 0x7fffffffLL)
+  // rows are numbered over all sequences and heads, in int32, up to the end of a row group (128 at most) behind the last
+  if ((long long)s->n_seq * s->n_head * chunk->max_new > 0x7fffffffLL - 255)
     return fail(SCALEKV_ERR_UNSUPPORTED, "n_seq * n_head * max_new = %lld is too large",
                 (long long)s->n_seq * s->n_head * chunk->max_new);
   return SCALEKV_OK;

@@ -365,6 +365,16 @@ def test_scales_may_lie_beside_the_codes_of_their_page(L):
     assert min(found) > 300, found
 
 
+def test_as_many_token_rows_as_the_kernels_can_count(L):
+    # rows of a unit are counted in int32, in row groups of up to 128: the last group's end has to fit
+    d, heads = 64, 64
+    pages = _pages(n_kv_head=1, head_stride=32 * d, page_stride=32 * d)
+    for new, status in (((2 ** 31 - 256) // heads, OK), ((2 ** 31 - 256) // heads + 1, UNSUPPORTED),
+                        ((2 ** 31 - 1) // d, UNSUPPORTED)):
+        st, need = _need(L, _shape(n_seq=1, n_head=heads, head_dim=d), pages, new)
+        assert st == status and (st != OK or need == 0) and (st == OK or "too large" in _err(L)), (new, st, need)
+
+
 # ---- the definitions in 64 bits that the GPU tests use
 
 def test_codes_are_the_nearest_e4m3_values_ties_to_even():
