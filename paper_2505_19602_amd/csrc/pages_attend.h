@@ -114,6 +114,9 @@ __device__ __forceinline__ Slice slice_of(const AttendArgs& a, unsigned wg) {
     s.len = __builtin_amdgcn_readlane(len, s.seq);
     s.count = __builtin_amdgcn_readlane(count, s.seq);
   } else {
+    // Each lane walks its share of the sequences, in every workgroup: work that grows with the square of their number.  Single
+    // tokens over 100 rows each, e4m3, 8 KV heads: 64 / 256 / 1024 / 2000 sequences 8.7 / 29 / 184 / 559 us, of which about none /
+    // 10 / 100 / 410 are this walk; over 600 rows 21 / 81 / 346 us for 64 / 256 / 1024.
     const int per_lane = (a.n_seq + 63) / 64, from = lane * per_lane, to = min(from + per_lane, a.n_seq);
     if (a.target) {
       double work = 0;

@@ -22,10 +22,12 @@
 // rows, then those from the window's first row on.
 //
 // What bounds it.  Few rows: HBM, each cached row being read once.  8 KV heads, head_dim 128, one token of 4 heads each: 64
-// sequences x 8000 rows bf16 361 us (5.8 TB/s), e4m3 194 us (5.5 TB/s); 2 x 131072 rows bf16 191 us (5.6 TB/s), e4m3 111 us; 64
-// sequences of up to 4000 rows, e4m3, 78 us (3.7 TB/s: the shortest workgroups are all start and end).  Small calls: the
-// chain length -> table -> rows -> products, and the join's launch: one sequence of 700 rows 10 us.  fp32, many rows: the
-// fp32 matrix rate, 24 units x 2048 causal tokens, head_dim 128, 411 us (63 TFLOP/s; a large product reaches 154).
+// sequences x 8000 rows bf16 352 us (6.0 TB/s), e4m3 190 us (5.6 TB/s); 2 x 131072 rows bf16 200 us (5.4 TB/s; fp32 378, 5.7 TB/s),
+// e4m3 113 us; 64 sequences of up to 4000 rows e4m3 78 us (3.7 TB/s: the shortest workgroups are all start and end), bf16 130 us
+// (4.4 TB/s), fp32 281 us (4.1 TB/s), fp32 over e4m3 224 us.  Small calls: the chain length -> table -> rows -> products, and the
+// join's launch: one sequence of 700 rows 10 us.  fp32, many rows: 24 units x 2048 causal tokens, head_dim 128, 409 us (63 TFLOP/s;
+// the dense fp32 kernel 104, a large product 154; over e4m3 415 us).  It is a chain, not a pipe, that bounds this: the matrix
+// pipe is busy for 46 % of the cycles, the LDS for 12 %, and waves wait 61 % of their time for an instruction to finish.
 //
 // Masked keys.  A weight of zero does not hide a value that is infinite or NaN from the product.  Rows hidden from all rows
 // of the workgroup are zeros in LDS; in the few tiles that some of its rows see and others do not (`edge`), values that
@@ -486,14 +488,21 @@ PagesPlan pages_plan(int dtype, int d, int n_seq, int n_head, const PagesView& p
   }
   // Rows of a workgroup.  Keys that 64 or 128 rows share are read once for them and their products fill the matrix cores; 16
   // rows leave more workgroups, whose waves split the keys.  A form is taken for units of more than `over` rows.  us with 16 /
-  // 64 / 128 rows to a workgroup, 128 units x 2000 rows of the cache, head_dim 128: bf16, units of 16 rows 38 / 34 / 41, 32 rows
-  // 42 / 39 / 46, 64 rows 56 / 41 / 48, 128 rows 103 / 49 / 54, 256 rows 189 / 79 / 69; e4m3, 32 rows 35 / 46 / 54, 48 rows 40 /
-  // 47 / 56, 64 rows 46 / 48 / 56, 128 rows 77 / 56 / 61, 256 rows 128 / 95 / 74.  (The form of 16 rows has the shortest start:
-  // 16 units of 4 rows x 2000 12.5 / 25 / 33.)  fp32, 16 / 64 rows, head_dim 64: 192 units x 2000 rows, 32 rows 68 / 120, 64 rows
-  // 105 / 125, 145 rows 254 / 260; 96 units of 1024 rows x 4000 1386 / 1048.
+  // 64 / 128 rows to a workgroup, 128 units x 2000 rows of the cache, head_dim 128: bf16, units of 4 rows 29 / 29 / 35, 16 rows 37 /
+  // 33 / 39, 32 rows 40 / 38 / 44, 64 rows 53 / 40 / 46, 128 rows 100 / 48 / 50, 256 rows 189 / 78 / 65; e4m3, 32 rows 33 / 45 / 52,
+  // 48 rows 38 / 46 / 54, 64 rows 45 / 46 / 54, 80 rows 55 / 54 / 56, 128 rows 76 / 56 / 57, 256 rows 127 / 95 / 70.  With few units
+  // the form of 16 rows, which has the shortest start, is ahead for longer: 16 units x 2000, 4 rows 12.5 / 25 / 33, 16 rows 19 /
+  // 28 / 36, 32 rows 21 / 33 / 41, e4m3 64 rows 28 / 43 / 51.  A line of `over` is one number between the two: beside it the form
+  // that is taken is up to 12 % behind (bf16 16 rows in many units), more often 4 %.  fp32, 16 / 64 rows, head_dim 64: 192 units x
+  // 2000 rows, 32 rows 68 / 121, 64 rows 105 / 125, 80 rows 153 / 158, 100 rows 192 / 162, 145 rows 253 / 260 (both forms step with
+  // the row groups that they fill), 256 rows 358 / 295; 96 units of 1024 rows x 4000 1232 / 1009.
   // Fewer rows, too, where compute units would be left without work and the keys, in pieces of min_tiles tiles, do not give
-  // them any: bf16, 16 units x 6000 rows, 32 rows 28 / 37 / 46, 256 rows 73 / 45 / 50; fp32, where only rows count: 24 units of
+  // them any: bf16, 16 units x 6000 rows, 32 rows 27 / 36 / 44, 256 rows 72 / 44 / 48; fp32, where only rows count: 24 units of
   // 145 rows x 585 20 / 44.
+  // Lengths are not known here: pieces of keys are counted up to the table's width.  Sequences far shorter than their table get
+  // more rows to a workgroup than they would under a table of their own length, and fewer workgroups: 64 tokens of one
+  // sequence over 600 rows, 8 KV heads, table for 131072 rows 28 us, for 600 rows 15 us (e4m3 33 and 15); 256 tokens of four
+  // over 2000 rows 62 either way.
   struct Rows {
     int waves, tiles, over;
   };

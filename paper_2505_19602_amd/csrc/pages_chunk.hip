@@ -13,11 +13,15 @@
 // the accumulators are rescaled behind the product that is then still to come with the old offset.
 //
 // What bounds it: the matrix cores and the softmax beside them, as in the dense kernel.  128 units x 4096 tokens x 4420 rows,
-// head_dim 128: bf16 1190 us (1.0 PFLOP/s; the dense kernel 1003 to 1050), causal 770 us, e4m3 1425 us (the codes' widening is
-// on top), head_dim 64 690 us (e4m3 828).  2048 tokens of 32 heads in a window of 1024 104 us (0.66 PFLOP/s): a walk is 17
-// tiles, of which the first and the last are masked element by element, and its start and end weigh.  4 ragged sequences of
-// up to 512 tokens over up to 8192 rows, e4m3 200 us (0.56 PFLOP/s), bf16 168 us: walks of 16 tiles and more, their sums through
-// the workspace, and 20 us of the join.
+// head_dim 128: bf16 1185 to 1220 us (cards differ; 1.0 PFLOP/s; the dense kernel 1046 where this takes 1213), causal 788 us, e4m3
+// 1510 us (the codes' widening is on top), head_dim 64 714 us (e4m3 858).  The first twenty passes after an idle chip take up
+// to a quarter longer.  The map keeps the matrix pipe busy for 46 % of its cycles, 38 % of those beside vector instructions,
+// of which there are 2.6 to an MFMA (e4m3 4.3), and the LDS for 24 %, 1 % of that in bank conflicts; e4m3 36 % and 23 %: the widened
+// rows' stores conflict.  2048 tokens of 32 heads in a window of 1024 105 us (0.65 PFLOP/s; e4m3 125): a walk is 18 tiles, one
+// for the sinks, and three of them are masked element by element; its start and end weigh (matrix pipe busy 32 %).  The
+// lookup by lengths at a workgroup's start costs 0.6 % of the map and 1 us of the window (measured with the lengths as
+// constants).  4 ragged sequences of up to 512 tokens over up to 8192 rows, e4m3 200 to 206 us (0.55 PFLOP/s), bf16 170 us: walks
+// of 16 tiles and more, their sums through the workspace (75 MB), and 17 us of the join.
 #include <type_traits>
 
 #include "pages_attend.h"

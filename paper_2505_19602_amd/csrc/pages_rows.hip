@@ -10,9 +10,10 @@
 // by that.  Lanes take 8 elements each (copies: 16 bytes), a row is covered by consecutive lanes, and all rows of the wave
 // are under way at once.  Rows that a list names are looked up one by one.
 //
-// head_dim 128: 256 units x 2304 rows bf16 into e4m3 79 to 90 us (5.3 to 5.8 TB/s; with places worked out by lanes 129), as they
-// are 118 us (5.1 TB/s); 256 units x 3350 rows back out of e4m3 117 us (5.6 TB/s; 191), out of bf16 151 us (5.8 TB/s).  A
-// large copy reaches 5.1 TB/s.  Listed rows, 60 units x 433 of head_dim 64, 4.9 us, 48 times as many units 40 us (5.3 TB/s).
+// head_dim 128: 256 units x 2304 rows bf16 into e4m3 79 to 90 us (5.8 to 5.0 TB/s; over two or many buffers in turn; with places
+// worked out by lanes 129), as they are 118 us (5.1 TB/s); 256 units x 3350 rows back out of e4m3 118 us (5.6 TB/s; 191), out of
+// bf16 151 us (5.8 TB/s).  A large copy reaches 5.1 TB/s.  Listed rows, 60 units x 433 of head_dim 64, 5 us, 16 times as many
+// units 40 us (5.3 TB/s), 48 times 126 us (5.1 TB/s).
 #include <type_traits>
 
 #include "pages.h"
