@@ -703,7 +703,8 @@ def _rows(t: torch.Tensor, shape: Shape, heads: int, name: str) -> _CRows:
 def pages_write(shape: Shape, pages: Pages, k_new: torch.Tensor, v_new: torch.Tensor,
                 first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
                 max_new: Optional[int] = None) -> None:
-    """scalekv_pages_write: rows of new tokens, [S, KV heads, n, d] or packed [N, KV heads, d], into their pages."""
+    """scalekv_pages_write: rows of new tokens, [S, KV heads, n, d] or packed [N, KV heads, d], into their pages.  With `first`
+    (packed tensors, padded batches) k_new and v_new have the same number of rows."""
     r = _marshaller().pages_write(shape, pages, k_new, v_new, first, count, max_new)
     if r is not None:
         _checked(r)
@@ -749,7 +750,7 @@ def pages_attend(shape: Shape, pages: Pages, q: torch.Tensor, out: torch.Tensor,
                  count: Optional[torch.Tensor] = None, max_new: Optional[int] = None) -> None:
     """scalekv_pages_attend: q, out [S,H,n,d] or packed [N,H,d]; the new tokens attend over the rows of their sequences,
     themselves included.  causal: up to a token's own position; window: only the last `window` of those, and the
-    first n_sink rows of the cache."""
+    first n_sink rows of the cache.  With `first` q and out have the same number of rows, each of one sequence."""
     r = _marshaller().pages_attend(shape, pages, q, out, ws, causal, window, n_sink, first, count, max_new)
     if r is not None:
         _checked(r)

@@ -212,3 +212,23 @@ def test_rows_of_out_that_lie_between_each_other(dtype, cache_dtype):
     assert torch.all(flat[[1, 8]] == 7.0)
     with pytest.raises(skv.ScaleKVError, match="coincide"):
         _run(skv.Shape(1, 2, d, dtype), cache.on(DEV), q.to(DEV), flat.as_strided((1, 2, new, d), (10 * d, 2 * d, 2 * d, 1)), new)
+
+
+def test_the_binding_refuses_lengths_and_rows_that_do_not_fit_each_other():
+    S, H, d, dtype = 2, 4, 64, BF16
+    shape, pages = skv.Shape(S, H, d, dtype), P.Cache(1, [20, 30], 2, d, 16, E4M3, dtype).on(DEV)
+    rows = lambda n, h: torch.zeros(n, h, d, dtype=dtype, device=DEV)
+    ws = torch.empty(skv.pages_workspace_bytes(shape, pages, 3), dtype=torch.uint8, device=DEV)
+    first = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    bits = [t.view(torch.uint8).clone() for t in (pages.k, pages.v)]
+    for a, b in ((6, 4), (4, 6), (6, 0)):
+        with pytest.raises(skv.ScaleKVError, match=f"k_new has {a} rows and v_new {b}"):
+            skv.pages_write(shape, pages, rows(a, 2), rows(b, 2), first=first, max_new=3)
+        with pytest.raises(skv.ScaleKVError, match=f"q has {a} rows and out {b}"):
+            skv.pages_attend(shape, pages, rows(a, H), rows(b, H), ws, first=first, max_new=3)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, t.view(torch.uint8)) for x, t in zip(bits, (pages.k, pages.v)))
+    table = pages.table.tolist()
+    skv.pages_check(shape, pages, table, [20, 30], first=[0, 3], max_new=3, n_row=6, packed=True)
+    with pytest.raises(skv.ScaleKVError, match="sequences 0 and 1 share row 2"):
+        skv.pages_check(shape, pages, table, [20, 30], first=[0, 2], max_new=3, n_row=6, packed=True)
