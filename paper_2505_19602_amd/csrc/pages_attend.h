@@ -115,8 +115,8 @@ __device__ __forceinline__ Slice slice_of(const AttendArgs& a, unsigned wg) {
     s.count = __builtin_amdgcn_readlane(count, s.seq);
   } else {
     // Each lane walks its share of the sequences, in every workgroup: work that grows with the square of their number.  Single
-    // tokens over 100 rows each, e4m3, 8 KV heads: 64 / 256 / 1024 / 2000 sequences 8.7 / 29 / 184 / 559 us, of which about none /
-    // 10 / 100 / 410 are this walk; over 600 rows 21 / 81 / 346 us for 64 / 256 / 1024.
+    // tokens over 100 rows each, e4m3, 8 KV heads: 65 / 256 / 1024 / 2000 sequences 10.7 / 29 / 184 / 559 us, with the lengths as
+    // constants 10.3 / 25 / 92 / 172; over 600 rows 25 / 81 / 345 (23 / 76 / 273) us for 65 / 256 / 1024.
     const int per_lane = (a.n_seq + 63) / 64, from = lane * per_lane, to = min(from + per_lane, a.n_seq);
     if (a.target) {
       double work = 0;
